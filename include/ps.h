@@ -393,6 +393,109 @@ ps_status ps_verify_static(int vocab, int B, int n_draft, int n_target, const in
                            int* out_tokens, int* n_out, int* nonfinite_flag, char* err,
                            size_t err_cap, void* stream);
 
+/* ---- Training operators --------------------------------------------------------------------
+ * The parts of a drafter's training step that know the group-wise layout or the vocabulary (Sec. 4.1
+ * "Group-wise Parallel Training"; Sec. 4.3: cross entropy against the target's LM head).  They need
+ * no context: the caller keeps weights, activations and gradients, the current CUDA device is the one
+ * used, all device pointers are that device's, and scratch lives in a workspace of the call that
+ * may be reused by the next call on the same stream (calls that may overlap need one each).
+ * Common to all of them:
+ *   - dtype is PS_DTYPE_F32 or PS_DTYPE_BF16: the storage type of every tensor marked `dtype`; sums,
+ *     softmax statistics and losses are float.  Row strides (ld*) count elements.
+ *   - outputs overlap neither inputs nor each other.  Rows that belong to no sequence, and columns
+ *     between a row's width and its stride, are left as they are.
+ *   - results do not depend on what else runs, nor from one run to the next.
+ *   - status   device [1] int or NULL: bit 1 is OR-ed in when a bounded device-side wait expired and
+ *              the outputs are not to be used (the caller zeroes it beforehand)
+ *   - err      host buffer for an error text, or NULL;  err_cap its size in bytes
+ *   - workspace device memory of at least the *_workspace_bytes() of the same sizes, 256-byte
+ *              aligned (PS_ERR_CAPACITY if smaller, PS_ERR_INVALID_ARG if misaligned) */
+
+/* Attention under the mask of parallel groups, forward and backward (the mask of ps_group_forward).
+ * B sequences lie one behind the other.  Sequence b has n_ctx[b] context positions, which lend
+ * their keys and values only, and n_groups[b] groups of R = k_masks + 1 rows: a real position and its
+ * k_masks [MASK] positions.  q, out, dout, dq and lse hold the group rows (sum of n_groups[b] * R),
+ * k, v, dk and dv the context and then the group rows of every sequence.  Row j of group t sees the
+ * context, row 0 of the groups 0..t and the rows 1..j of its own group: with k_masks = 0 this is causal
+ * attention.  With s_rc = scale * q_r . k_c over the keys c that r sees,
+ *   lse_r = log sum_c exp(s_rc),  p_rc = exp(s_rc - lse_r),  out_r = sum_c p_rc v_c
+ *   dv_c = sum_r p_rc dout_r,  ds_rc = p_rc (dout_r . v_c - dout_r . out_r),
+ *   dq_r = scale sum_c ds_rc k_c,  dk_c = scale sum_r ds_rc q_r
+ * where a key head's sums run over all query heads that share it.  q and k are as they are after the
+ * rotation (row j of group t stands at position n_ctx + t + j).  The backward pass forms p again from q, k and lse.
+ * A key or value that a row does not see does not touch that row, whatever its bits are.
+ * Rows are [heads][head_dim], dense within a row; any row stride of at least that width. */
+typedef struct ps_group_attn_args {
+  int dtype;            /* PS_DTYPE_* */
+  int B;                /* sequences, 1..PS_MAX_BATCH */
+  int k_masks;          /* 0..PS_MAX_MASKS */
+  int n_heads;          /* query heads, at most 1024 */
+  int n_kv_heads;       /* divides n_heads */
+  int head_dim;         /* 64 or 128 */
+  const int* n_ctx;     /* host [B], >= 0; read during the call */
+  const int* n_groups;  /* host [B], >= 0 */
+  float scale;          /* finite */
+  const void *q, *k, *v;             /* dtype */
+  size_t ldq, ldk, ldv;
+  void* out;                         /* dtype; written by the forward call, read by the backward call */
+  size_t ldo;
+  float* lse;                        /* [n_heads][group rows]; written forward, read backward */
+  const void* dout;                  /* dtype; backward only, like the rest */
+  size_t lddo;
+  void *dq, *dk, *dv;                /* dtype */
+  size_t lddq, lddk, lddv;
+} ps_group_attn_args;
+
+/* Bytes of workspace of one call with these sizes (pointers and strides are not looked at), 0 if the
+ * sizes are invalid.  backward: 0 or 1. */
+size_t ps_group_attn_workspace_bytes(const ps_group_attn_args* a, int backward);
+ps_status ps_group_attn(const ps_group_attn_args* a, void* workspace, size_t workspace_bytes, int* status,
+                        char* err, size_t err_cap, void* stream);
+ps_status ps_group_attn_backward(const ps_group_attn_args* a, void* workspace, size_t workspace_bytes,
+                                 int* status, char* err, size_t err_cap, void* stream);
+
+/* Softmax cross entropy of the LM head, forward and backward, over pieces of the vocabulary: the logits
+ * x w^T (in single precision) never exist as a whole.
+ *   lse_i = log sum_v exp(x_i . w_v),  loss_i = lse_i - x_i . w_label(i)
+ *   g_iv = dloss_i (exp(x_i . w_v - lse_i) - [v = label(i)]),  dx_i = sum_v g_iv w_v,  dw_v = sum_i g_iv x_i
+ * A row whose label lies outside [0, vocab) (such as -100) counts for nothing: its loss, lse and dx are
+ * 0, it adds nothing to dw, and neither its x nor its dloss is read.
+ *   x, dx    device [rows][hidden] dtype, row strides ldx and lddx
+ *   w, dw    device [vocab][hidden] dtype, dense
+ *   labels   device [rows] int32
+ *   loss, lse device [rows] float (the backward call reads lse)
+ *   dloss    device [rows] float: gradient of the caller's scalar with respect to each row's loss
+ *   dx, dw   either may be NULL: that gradient is not formed
+ * hidden is a multiple of 8 (PS_ERR_UNSUPPORTED otherwise, and for a w or dw off a 16-byte boundary);
+ * vocab <= 2^20, rows <= 2^20.  rows = 0 is allowed (dw is then set to zero). */
+size_t ps_lm_loss_workspace_bytes(int dtype, int rows, int hidden, int vocab, int backward);
+ps_status ps_lm_loss(int dtype, int rows, int hidden, int vocab, const void* x, size_t ldx, const void* w,
+                     const int* labels, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                     int* status, char* err, size_t err_cap, void* stream);
+ps_status ps_lm_loss_backward(int dtype, int rows, int hidden, int vocab, const void* x, size_t ldx,
+                              const void* w, const int* labels, const float* lse, const float* dloss, void* dx,
+                              size_t lddx, void* dw, void* workspace, size_t workspace_bytes, int* status,
+                              char* err, size_t err_cap, void* stream);
+
+/* Input rows of a step, and the gradients of what they were taken from.
+ *   out_r = scale * table[id]            0 <= id < vocab
+ *           scale * mask_rows[id-vocab]  vocab <= id < vocab + k_masks: the [MASK] rows (Sec. 4.3)
+ *           0                            any other id (a padded row)
+ *   d_table[v] = scale * sum of dout_r over the rows r with id v, d_mask likewise; rows of the table
+ *   that no id names are set to 0.  The rows of an id are added in increasing order (in pieces of 32).
+ *   ids      device [rows] int32;  out, dout device [rows][hidden] dtype, row strides ldo and lddo
+ *   table, d_table device [vocab][hidden] dtype, mask_rows, d_mask device [k_masks][hidden] dtype, dense
+ *   d_table, d_mask: either may be NULL: that gradient is not formed.  mask_rows may be NULL if k_masks = 0
+ * rows <= 2^24, hidden <= 65536, vocab <= 2^20, k_masks <= PS_MAX_MASKS; any alignment of the element type. */
+ps_status ps_embed_rows(int dtype, int rows, int hidden, int vocab, int k_masks, const int* ids,
+                        const void* table, const void* mask_rows, float scale, void* out, size_t ldo,
+                        char* err, size_t err_cap, void* stream);
+size_t ps_embed_rows_workspace_bytes(int dtype, int rows, int hidden, int vocab, int k_masks);
+ps_status ps_embed_rows_backward(int dtype, int rows, int hidden, int vocab, int k_masks, const int* ids,
+                                 float scale, const void* dout, size_t lddo, void* d_table, void* d_mask,
+                                 void* workspace, size_t workspace_bytes, char* err, size_t err_cap,
+                                 void* stream);
+
 #ifdef __cplusplus
 }
 #endif

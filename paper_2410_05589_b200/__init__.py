@@ -10,6 +10,12 @@ from .binding import (  # noqa: F401
     PS_FLAG_UNFUSED_KERNELS,
     Drafter,
     PsError,
+    embed_rows,
+    embed_rows_backward,
+    group_attention,
+    group_attention_backward,
+    lm_loss,
+    lm_loss_backward,
     load_library,
     philox_fill,
     verify_static,

@@ -33,6 +33,8 @@ EXPORTS = (
     "ps_verify_static", "ps_debug_buffer", "ps_verify_tree", "ps_draft_step_sampled", "ps_group_forward",
     "ps_build_tree", "ps_debug_wait_expires", "ps_debug_check_guards", "ps_debug_late_copy",
     "ps_debug_gemm_plan", "ps_debug_append_pass_rows",
+    "ps_group_attn_workspace_bytes", "ps_group_attn", "ps_group_attn_backward", "ps_lm_loss_workspace_bytes",
+    "ps_lm_loss", "ps_lm_loss_backward", "ps_embed_rows", "ps_embed_rows_workspace_bytes", "ps_embed_rows_backward",
 )
 
 
@@ -53,6 +55,18 @@ class ps_config(C.Structure):
 
 class ps_weights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in WEIGHT_NAMES]
+
+
+class ps_group_attn_args(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int), ("B", C.c_int), ("k_masks", C.c_int), ("n_heads", C.c_int), ("n_kv_heads", C.c_int),
+        ("head_dim", C.c_int), ("n_ctx", C.POINTER(C.c_int)), ("n_groups", C.POINTER(C.c_int)), ("scale", C.c_float),
+        ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+        ("ldq", C.c_size_t), ("ldk", C.c_size_t), ("ldv", C.c_size_t),
+        ("out", C.c_void_p), ("ldo", C.c_size_t), ("lse", C.c_void_p), ("dout", C.c_void_p), ("lddo", C.c_size_t),
+        ("dq", C.c_void_p), ("dk", C.c_void_p), ("dv", C.c_void_p),
+        ("lddq", C.c_size_t), ("lddk", C.c_size_t), ("lddv", C.c_size_t),
+    ]
 
 
 _lib = None
@@ -105,6 +119,19 @@ def load_library(path: str | None = None) -> C.CDLL:
     lib.ps_debug_buffer.argtypes = [vp, C.c_char_p, C.POINTER(vp), C.POINTER(C.c_size_t)]
     lib.ps_verify_static.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_float,
                                      C.c_uint64, C.c_uint64, vp, vp, vp, vp, C.c_char_p, C.c_size_t, vp]
+    ga, sz, f = C.POINTER(ps_group_attn_args), C.c_size_t, C.c_float
+    lib.ps_group_attn_workspace_bytes.restype = sz
+    lib.ps_group_attn_workspace_bytes.argtypes = [ga, C.c_int]
+    lib.ps_group_attn.argtypes = [ga, vp, sz, vp, C.c_char_p, sz, vp]
+    lib.ps_group_attn_backward.argtypes = [ga, vp, sz, vp, C.c_char_p, sz, vp]
+    lib.ps_lm_loss_workspace_bytes.restype = sz
+    lib.ps_lm_loss_workspace_bytes.argtypes = [C.c_int] * 5
+    lib.ps_lm_loss.argtypes = [C.c_int] * 4 + [vp, sz, vp, vp, vp, vp, vp, sz, vp, C.c_char_p, sz, vp]
+    lib.ps_lm_loss_backward.argtypes = [C.c_int] * 4 + [vp, sz, vp, vp, vp, vp, vp, sz, vp, vp, sz, vp, C.c_char_p, sz, vp]
+    lib.ps_embed_rows.argtypes = [C.c_int] * 5 + [vp, vp, vp, f, vp, sz, C.c_char_p, sz, vp]
+    lib.ps_embed_rows_workspace_bytes.restype = sz
+    lib.ps_embed_rows_workspace_bytes.argtypes = [C.c_int] * 5
+    lib.ps_embed_rows_backward.argtypes = [C.c_int] * 5 + [vp, f, vp, sz, vp, vp, vp, sz, C.c_char_p, sz, vp]
     _lib = lib
     return lib
 
@@ -176,6 +203,260 @@ def verify_static(draft_tokens: torch.Tensor, draft_logits, target_logits: torch
     if rc != PS_OK:
         raise PsError(rc, err.value.decode())
     return out
+
+
+# ---- training operators ----------------------------------------------------------------------------
+# Functions of tensors: they need no Drafter.  Outputs and workspaces are allocated per call on the stream the
+# call runs on (pass ``out`` to reuse outputs), so that calls on several streams and captured graphs share nothing.
+_DTYPE_CODE = {torch.float32: PS_DTYPE_F32, torch.bfloat16: PS_DTYPE_BF16}
+
+
+class _on:
+    """Makes the tensors' device current, and ``stream`` where one is given."""
+
+    def __init__(self, device, stream):
+        self.ctx = []
+        if device.index is not None and device.index != _device():
+            self.ctx.append(torch.cuda.device(device))
+        if stream is not None:
+            self.ctx.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for c in self.ctx:
+            c.__enter__()
+
+    def __exit__(self, *exc):
+        for c in reversed(self.ctx):
+            c.__exit__(*exc)
+
+
+def _need(ok, text):
+    if not ok:
+        raise PsError(-1, text)
+
+
+def _tensors(first, *others, dtype=None):
+    """CUDA tensors of one device (None is skipped) and, with ``dtype``, of one type."""
+    _need(first.is_cuda, "tensors must lie on a CUDA device")
+    for t in (first, *others):
+        if t is not None:
+            _need(t.device == first.device, "tensors lie on different devices")
+            _need(dtype is None or t.dtype == dtype, f"expected {dtype}, got {t.dtype}")
+
+
+def _rows(t, width, name):
+    """Row stride in elements of a tensor of rows that are dense; a view of a wider buffer may have a larger one."""
+    w = 1
+    for n, s in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        _need(n == 1 or s == w, f"{name}: rows must be dense")
+        w *= n
+    _need(w == width, f"{name}: rows of {w} values, expected {width}")
+    if t.shape[0] <= 1:
+        return width
+    _need(t.stride(0) >= width, f"{name}: rows overlap")
+    return t.stride(0)
+
+
+def _op(fn, *args):
+    err = C.create_string_buffer(256)
+    rc = fn(*args, err, 256, _stream())
+    if rc != PS_OK:
+        raise PsError(rc, err.value.decode())
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _scratch(nbytes, device):
+    _need(nbytes > 0, "sizes out of range")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _group_args(q, k, v, n_ctx, n_groups, k_masks, scale):
+    _tensors(q, k, v, dtype=q.dtype)
+    _need(q.dtype in _DTYPE_CODE, f"q: float32 or bfloat16, got {q.dtype}")
+    _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.shape[2] == q.shape[2],
+          "q [rows][n_heads][head_dim], k and v [rows][n_kv_heads][head_dim]")
+    _need(len(n_ctx) == len(n_groups), "n_ctx and n_groups have one entry per sequence")
+    n_ctx, n_groups = [int(x) for x in n_ctx], [int(x) for x in n_groups]
+    rows = sum(n_groups) * (k_masks + 1)
+    _need(q.shape[0] == rows and k.shape[0] == rows + sum(n_ctx), "the rows do not add up to the sequences")
+    d = q.shape[2]
+    a = ps_group_attn_args()
+    a.dtype, a.B, a.k_masks = _DTYPE_CODE[q.dtype], len(n_ctx), k_masks
+    a.n_heads, a.n_kv_heads, a.head_dim = q.shape[1], k.shape[1], d
+    a.n_ctx, a.n_groups = _iarr(n_ctx), _iarr(n_groups)
+    a.scale = d ** -0.5 if scale is None else float(scale)
+    wq, wk = q.shape[1] * d, k.shape[1] * d
+    a.q, a.k, a.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
+    a.ldq, a.ldk, a.ldv = _rows(q, wq, "q"), _rows(k, wk, "k"), _rows(v, wk, "v")
+    a.ldo, a.lddo, a.lddq, a.lddk, a.lddv = wq, wq, wq, wk, wk
+    return a
+
+
+def group_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_ctx, n_groups, k_masks: int, scale=None,
+                    out: dict | None = None, status=None, stream=None) -> dict:
+    """ps_group_attn: attention under the mask of parallel groups.
+
+    q [group rows][n_heads][head_dim]; k, v [context and group rows][n_kv_heads][head_dim], float32 or bfloat16, views
+    with a larger row stride allowed; n_ctx, n_groups: host lists, one entry per sequence; scale: head_dim ** -0.5 by
+    default.  Returns ``out`` (like q) and ``lse`` [n_heads][group rows] float32; ``out`` may carry them preallocated.
+    """
+    a = _group_args(q, k, v, n_ctx, n_groups, k_masks, scale)
+    lib = load_library()
+    with _on(q.device, stream):
+        o = out if out is not None else {}
+        if "out" not in o:
+            o["out"] = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if "lse" not in o:
+            o["lse"] = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+        _tensors(q, o["out"], dtype=q.dtype)
+        _tensors(q, o["lse"], status)
+        _need(o["out"].shape == q.shape and o["lse"].dtype == torch.float32 and o["lse"].is_contiguous() and
+              tuple(o["lse"].shape) == (q.shape[1], q.shape[0]), "out like q, lse [n_heads][rows] float32")
+        a.out, a.lse, a.ldo = o["out"].data_ptr(), o["lse"].data_ptr(), _rows(o["out"], q.shape[1] * q.shape[2], "out")
+        n = lib.ps_group_attn_workspace_bytes(C.byref(a), 0)
+        ws = _scratch(n, q.device) if n else None   # (0: the call says why)
+        _op(lib.ps_group_attn, C.byref(a), _ptr(ws), n, _ptr(status))
+    return o
+
+
+def group_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                             lse: torch.Tensor, n_ctx, n_groups, k_masks: int, scale=None, grads: dict | None = None,
+                             status=None, stream=None) -> dict:
+    """ps_group_attn_backward: ``dq``, ``dk``, ``dv`` (like q, k, v) from dout, with out and lse of the forward call.
+    ``grads`` may carry them preallocated, as views of wider buffers too."""
+    a = _group_args(q, k, v, n_ctx, n_groups, k_masks, scale)
+    lib = load_library()
+    wq, wk = q.shape[1] * q.shape[2], k.shape[1] * k.shape[2]
+    with _on(q.device, stream):
+        o = grads if grads is not None else {}
+        for name, like in (("dq", q), ("dk", k), ("dv", v)):
+            if name not in o:
+                o[name] = torch.empty(like.shape, dtype=q.dtype, device=q.device)
+            _need(o[name].shape == like.shape, f"{name} has another shape than its tensor")
+        _tensors(q, dout, out, o["dq"], o["dk"], o["dv"], dtype=q.dtype)
+        _tensors(q, lse, status)
+        _need(dout.shape == q.shape and out.shape == q.shape, "dout and out like q")
+        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[1], q.shape[0]),
+              "lse [n_heads][rows] float32")
+        a.out, a.lse, a.dout = out.data_ptr(), lse.data_ptr(), dout.data_ptr()
+        a.ldo, a.lddo = _rows(out, wq, "out"), _rows(dout, wq, "dout")
+        a.dq, a.dk, a.dv = o["dq"].data_ptr(), o["dk"].data_ptr(), o["dv"].data_ptr()
+        a.lddq, a.lddk, a.lddv = _rows(o["dq"], wq, "dq"), _rows(o["dk"], wk, "dk"), _rows(o["dv"], wk, "dv")
+        n = lib.ps_group_attn_workspace_bytes(C.byref(a), 1)
+        ws = _scratch(n, q.device) if n else None
+        _op(lib.ps_group_attn_backward, C.byref(a), _ptr(ws), n, _ptr(status))
+    return o
+
+
+def _loss_args(x, w, labels):
+    _tensors(x, w, dtype=x.dtype)
+    _tensors(x, labels, dtype=None)
+    _need(x.dtype in _DTYPE_CODE, f"x: float32 or bfloat16, got {x.dtype}")
+    _need(x.dim() == 2 and w.dim() == 2 and w.shape[1] == x.shape[1] and w.is_contiguous(), "x [rows][hidden], w [vocab][hidden] dense")
+    _need(labels.dtype == torch.int32 and labels.is_contiguous() and tuple(labels.shape) == (x.shape[0],), "labels [rows] int32")
+    return _DTYPE_CODE[x.dtype], x.shape[0], x.shape[1], w.shape[0]
+
+
+def lm_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, out: dict | None = None, status=None,
+            stream=None) -> dict:
+    """ps_lm_loss: softmax cross entropy of the logits x w^T, which never exist as a whole.
+
+    x [rows][hidden] (a view with a larger row stride allowed), w [vocab][hidden], float32 or bfloat16; labels [rows]
+    int32, any value outside the vocabulary (-100) for rows that count for nothing.  Returns ``loss`` and ``lse``
+    [rows] float32, 0 for those rows."""
+    size = _loss_args(x, w, labels)
+    lib = load_library()
+    with _on(x.device, stream):
+        o = out if out is not None else {}
+        for name in ("loss", "lse"):
+            if name not in o:
+                o[name] = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+            _need(o[name].dtype == torch.float32 and o[name].is_contiguous() and o[name].shape == labels.shape, f"{name} [rows] float32")
+        _tensors(x, o["loss"], o["lse"], status)
+        n = lib.ps_lm_loss_workspace_bytes(*size, 0)
+        ws = _scratch(n, x.device) if n else None
+        _op(lib.ps_lm_loss, *size, _ptr(x), _rows(x, x.shape[1], "x"), _ptr(w), _ptr(labels), _ptr(o["loss"]), _ptr(o["lse"]),
+            _ptr(ws), n, _ptr(status))
+    return o
+
+
+def lm_loss_backward(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                     want_dx: bool = True, want_dw: bool = True, grads: dict | None = None, status=None,
+                     stream=None) -> dict:
+    """ps_lm_loss_backward: ``dx`` (like x) and ``dw`` (like w) from dloss [rows] float32, the gradient of the caller's
+    scalar with respect to each row's loss (1 / rows that count, for their mean), and lse of the forward call.
+    ``grads`` may carry them preallocated."""
+    size = _loss_args(x, w, labels)
+    lib = load_library()
+    with _on(x.device, stream):
+        o = grads if grads is not None else {}
+        for name, like, want in (("dx", x, want_dx), ("dw", w, want_dw)):
+            if want and name not in o:
+                o[name] = torch.empty(like.shape, dtype=x.dtype, device=x.device)
+        dx, dw = o.get("dx") if want_dx else None, o.get("dw") if want_dw else None
+        _tensors(x, dx, dw, dtype=x.dtype)
+        _tensors(x, lse, dloss, status)
+        for t in (lse, dloss):
+            _need(t.dtype == torch.float32 and t.is_contiguous() and t.shape == labels.shape, "lse and dloss [rows] float32")
+        _need(dx is None or dx.shape == x.shape, "dx like x")
+        _need(dw is None or (dw.shape == w.shape and dw.is_contiguous()), "dw like w, dense")
+        n = lib.ps_lm_loss_workspace_bytes(*size, 1)
+        ws = _scratch(n, x.device) if n else None
+        _op(lib.ps_lm_loss_backward, *size, _ptr(x), _rows(x, x.shape[1], "x"), _ptr(w), _ptr(labels), _ptr(lse), _ptr(dloss),
+            _ptr(dx), x.shape[1] if dx is None else _rows(dx, x.shape[1], "dx"), _ptr(dw), _ptr(ws), n, _ptr(status))
+    return o
+
+
+def embed_rows(ids: torch.Tensor, table: torch.Tensor, mask_rows=None, scale: float = 1.0, out=None,
+               stream=None) -> torch.Tensor:
+    """ps_embed_rows: scaled rows of table [vocab][hidden] (ids below vocab) and of mask_rows [k_masks][hidden] (ids from
+    vocab on); any other id gives a row of zeros.  ids [rows] int32; ``out`` [rows][hidden] may be a view with a
+    larger row stride, such as the embedding half of the fc layer's input."""
+    _tensors(table, mask_rows, out, dtype=table.dtype)
+    _tensors(table, ids)
+    _need(table.dtype in _DTYPE_CODE, f"table: float32 or bfloat16, got {table.dtype}")
+    _need(table.dim() == 2 and table.is_contiguous() and ids.dim() == 1 and ids.dtype == torch.int32 and ids.is_contiguous(),
+          "table [vocab][hidden] dense, ids [rows] int32")
+    V, H = table.shape
+    _need(mask_rows is None or (mask_rows.dim() == 2 and mask_rows.shape[1] == H and mask_rows.is_contiguous()), "mask_rows [k_masks][hidden] dense")
+    lib = load_library()
+    with _on(table.device, stream):
+        if out is None:
+            out = torch.empty((ids.shape[0], H), dtype=table.dtype, device=table.device)
+        _need(tuple(out.shape) == (ids.shape[0], H), "out [rows][hidden]")
+        _op(lib.ps_embed_rows, _DTYPE_CODE[table.dtype], ids.shape[0], H, V, 0 if mask_rows is None else mask_rows.shape[0],
+            _ptr(ids), _ptr(table), _ptr(mask_rows), float(scale), _ptr(out), _rows(out, H, "out"))
+    return out
+
+
+def embed_rows_backward(ids: torch.Tensor, dout: torch.Tensor, vocab: int, k_masks: int = 0, scale: float = 1.0,
+                        want_table: bool = True, want_mask: bool = True, grads: dict | None = None, stream=None) -> dict:
+    """ps_embed_rows_backward: ``d_table`` [vocab][hidden] and ``d_mask`` [k_masks][hidden], the scaled sums of the rows of
+    dout [rows][hidden] per id, zeros for ids without a row.  ``grads`` may carry them preallocated."""
+    _tensors(dout, ids)
+    _need(dout.dtype in _DTYPE_CODE, f"dout: float32 or bfloat16, got {dout.dtype}")
+    _need(dout.dim() == 2 and ids.dtype == torch.int32 and ids.is_contiguous() and tuple(ids.shape) == (dout.shape[0],),
+          "dout [rows][hidden], ids [rows] int32")
+    n_rows, H = dout.shape
+    lib = load_library()
+    with _on(dout.device, stream):
+        o = grads if grads is not None else {}
+        for name, n, want in (("d_table", vocab, want_table), ("d_mask", k_masks, want_mask and k_masks > 0)):
+            if want:
+                if name not in o:
+                    o[name] = torch.empty((n, H), dtype=dout.dtype, device=dout.device)
+                _tensors(dout, o[name], dtype=dout.dtype)
+                _need(tuple(o[name].shape) == (n, H) and o[name].is_contiguous(), f"{name} [{n}][hidden] dense")
+        dt, dm = o.get("d_table") if want_table else None, o.get("d_mask") if want_mask and k_masks > 0 else None
+        code = _DTYPE_CODE[dout.dtype]
+        n = lib.ps_embed_rows_workspace_bytes(code, n_rows, H, vocab, k_masks)
+        ws = _scratch(n, dout.device) if n else None
+        _op(lib.ps_embed_rows_backward, code, n_rows, H, vocab, k_masks, _ptr(ids), float(scale), _ptr(dout), _rows(dout, H, "dout"),
+            _ptr(dt), _ptr(dm), _ptr(ws), n)
+    return o
 
 
 class Drafter:

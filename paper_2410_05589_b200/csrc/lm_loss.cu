@@ -1,0 +1,481 @@
+// Softmax cross entropy of the LM head (ps_lm_loss, ps_lm_loss_backward) over pieces of the vocabulary.
+//
+//   s = x W^T,  lse = log sum_v exp s_v,  loss = lse - s_label
+//   g = dloss (exp(s - lse) - onehot),    dx = g W,  dW = g^T x
+// Forward: each tile of the product x W^T leaves, per row, the maximum of its logits and the sum of their
+// exponentials against it (and the label's logit where it holds it); a small kernel joins the tiles.  Backward:
+// the logits of a piece of the vocabulary are formed again, turned into g by the epilogue of the product
+// that forms them and kept for the two products that use them.  dx is summed over the pieces in single
+// precision, dW of a piece is complete.
+// What bounds it: the products, 2 rows hidden vocab operations each (one forward, one to three backward).
+//
+// This file has the steps around the products, and the products of fp32 operands on the FMA units: 64 x 64
+// tiles, 4 x 4 sums a thread.  bf16 goes to the tensor cores (lm_loss_tc.cu).
+#include "lm_loss.cuh"
+
+namespace ps {
+namespace train {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---- rows that count -----------------------------------------------------------------------------
+// One block numbers them (a running sum over 1024 rows at a time).
+__global__ void __launch_bounds__(1024) k_loss_rows(int rows, int rows_pad, int V, const int* __restrict__ labels, LossBuf b,
+                                                    const float* __restrict__ lse_in, const float* __restrict__ dloss,
+                                                    float* loss, float* lse) {
+  __shared__ int s_w[32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_launch_dependents();
+  pdl_wait();
+  int base = 0;
+  for (int r0 = 0; r0 < rows; r0 += 1024) {
+    const int r = r0 + tid;
+    const int lab = r < rows ? labels[r] : -1;
+    const bool counts = lab >= 0 && lab < V;
+    const unsigned m = __ballot_sync(0xffffffffu, counts);
+    if (lane == 0) s_w[warp] = __popc(m);
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < 32; ++w) {
+      const int c = s_w[w];
+      if (w < warp) before += c;
+      all += c;
+    }
+    if (r < rows) {
+      const int i = counts ? base + before + __popc(m & ((1u << lane) - 1)) : -1;
+      b.slot[r] = i;
+      if (counts) {
+        b.row_of[i] = r;
+        b.label[i] = lab;
+        if (lse_in) {
+          b.lse[i] = lse_in[r];
+          b.up[i] = dloss[r];
+        }
+      } else if (loss) {
+        loss[r] = 0.f;
+        lse[r] = 0.f;
+      }
+    }
+    base += all;
+    __syncthreads();
+  }
+  if (tid == 0) *b.n = base;
+  for (int i = base + tid; i < rows_pad; i += 1024) {   // rows that only fill up a tile
+    b.label[i] = -1;
+    b.lse[i] = 0.f;
+    b.up[i] = 0.f;
+  }
+}
+
+// Compact copy of the rows that count, zeros up to the end of the last tile.  A block per row.
+template <class T>
+__global__ void __launch_bounds__(256) k_loss_gather(int H, int tile, const T* __restrict__ x, size_t ldx, LossBuf b, bool vec) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int n = *b.n, i = blockIdx.x;
+  if (i >= (n + tile - 1) / tile * tile) return;
+  constexpr int N = 16 / sizeof(T);
+  uint4* dst = reinterpret_cast<uint4*>((T*)b.x + (size_t)i * H);
+  if (i >= n) {
+    for (int c = threadIdx.x; c < H / N; c += 256) dst[c] = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  const T* src = x + (size_t)b.row_of[i] * ldx;
+  if (vec) {
+    for (int c = threadIdx.x; c < H / N; c += 256) dst[c] = reinterpret_cast<const uint4*>(src)[c];
+  } else {
+    for (int c = threadIdx.x; c < H; c += 256) ((T*)b.x)[(size_t)i * H + c] = src[c];
+  }
+}
+
+// Joins a row's tiles: a warp per compact row.
+__global__ void __launch_bounds__(256) k_loss_join(int rows_pad, int tiles, LossBuf b, float* loss, float* lse) {
+  pdl_wait();
+  const int i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (i >= *b.n) return;
+  float m = -INFINITY, s = 0.f;
+  bool nan = false;
+  for (int t = lane; t < tiles; t += 32) {
+    const float2 p = b.part[(size_t)t * rows_pad + i];
+    nan |= p.y != p.y;
+    if (p.x > m) {
+      s = s * exp2f((m - p.x) * kLog2e) + p.y;
+      m = p.x;
+    } else if (p.x > -INFINITY) {
+      s += p.y * exp2f((p.x - m) * kLog2e);
+    }
+  }
+  float top = m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  s = m > -INFINITY ? s * exp2f((m - top) * kLog2e) : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (__any_sync(0xffffffffu, nan)) s = NAN;
+  if (lane == 0) {
+    const float l = top + logf(s);
+    const int r = b.row_of[i];
+    lse[r] = l;
+    loss[r] = l - b.picked[i];
+  }
+}
+
+// dx of a row from its sums; a block per row.
+template <class T>
+__global__ void __launch_bounds__(256) k_loss_dx(int H, int splits, size_t layer, LossBuf b, T* dx, size_t ldx, bool vec) {
+  pdl_wait();
+  const int i = b.slot[blockIdx.x];
+  T* dst = dx + (size_t)blockIdx.x * ldx;
+  const float* a = b.acc + (size_t)(i < 0 ? 0 : i) * H;
+  for (int c = 4 * threadIdx.x; c < H; c += 1024) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i >= 0)
+      for (int k = 0; k < splits; ++k) {
+        const float4 y = *reinterpret_cast<const float4*>(a + k * layer + c);
+        s.x += y.x; s.y += y.y; s.z += y.z; s.w += y.w;
+      }
+    if constexpr (sizeof(T) == 4) {
+      if (vec) *reinterpret_cast<float4*>(dst + c) = s;
+      else { dst[c] = s.x; dst[c + 1] = s.y; dst[c + 2] = s.z; dst[c + 3] = s.w; }
+    } else {
+      const __nv_bfloat162 u = __floats2bfloat162_rn(s.x, s.y), v = __floats2bfloat162_rn(s.z, s.w);
+      if (vec) {
+        *reinterpret_cast<uint2*>(dst + c) = make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
+      } else {
+        dst[c] = u.x; dst[c + 1] = u.y; dst[c + 2] = v.x; dst[c + 3] = v.y;
+      }
+    }
+  }
+}
+
+// ---- products on the FMA units ---------------------------------------------------------------------
+constexpr int kT = 64, kBK = 32, kPitch = 68;
+
+// 64 x 64 tile of A B over k in [k0, k1): 256 threads, thread (ty, tx) has rows 4 ty + i and columns 4 tx + j.  An operand
+// is [mn][k] with k contiguous (KC) or [k][mn] with mn contiguous; mn_end: first row (column) that there is none of.  In
+// shared memory both are [k][mn], eight columns' place exchanged by k's bits 3 and 4 so that the transposing stores of
+// a warp (8 rows of 4 groups of k) fall on 32 banks.
+template <bool KC, class T>
+__device__ __forceinline__ void load8(const T* __restrict__ p, size_t ld, int mn0, int mn_end, int k0, int k1, float (&v)[8]) {
+  const int t = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  const int mn = KC ? mn0 + t / 4 : mn0 + (t % 8) * 8, k = KC ? k0 + (t % 4) * 8 : k0 + t / 8;
+  const T* q = KC ? p + (size_t)mn * ld + k : p + (size_t)k * ld + mn;
+  const int n = KC ? (mn < mn_end ? k1 - k : 0) : (k < k1 ? mn_end - mn : 0);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (n >= 4 * h + 4 && ld % 4 == 0) {
+      const float4 x = *reinterpret_cast<const float4*>(q + 4 * h);
+      v[4 * h] = x.x; v[4 * h + 1] = x.y; v[4 * h + 2] = x.z; v[4 * h + 3] = x.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (4 * h + i < n) v[4 * h + i] = q[4 * h + i];
+    }
+  }
+}
+template <bool KC>
+__device__ __forceinline__ void stage8(float* s, const float (&v)[8]) {
+  const int t = threadIdx.x;
+  if (KC) {
+    const int mn = (t / 4) ^ ((t % 4) * 8), k = (t % 4) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[(k + i) * kPitch + mn] = v[i];
+  } else {
+    const int k = t / 8, mn = ((t % 8) * 8) ^ (((k >> 3) & 3) * 8);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      *reinterpret_cast<float4*>(s + k * kPitch + mn + 4 * h) = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+  }
+}
+struct TileSmem { float a[kBK * kPitch], b[kBK * kPitch]; };
+
+template <bool AKC, bool BKC>
+__device__ __forceinline__ void tile_product(const float* A, size_t lda, int m0, int m_end, const float* B, size_t ldb, int n0,
+                                             int n_end, int k0, int k1, TileSmem& sm, float (&c)[4][4]) {
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[i][j] = 0.f;
+  float va[8], vb[8];
+  load8<AKC>(A, lda, m0, m_end, k0, k1, va);
+  load8<BKC>(B, ldb, n0, n_end, k0, k1, vb);
+  for (int k = k0; k < k1; k += kBK) {
+    __syncthreads();
+    stage8<AKC>(sm.a, va);
+    stage8<BKC>(sm.b, vb);
+    __syncthreads();
+    if (k + kBK < k1) {
+      load8<AKC>(A, lda, m0, m_end, k + kBK, k1, va);
+      load8<BKC>(B, ldb, n0, n_end, k + kBK, k1, vb);
+    }
+#pragma unroll
+    for (int kk = 0; kk < kBK; ++kk) {
+      const int sw = ((kk >> 3) & 3) * 8;
+      const float4 x = *reinterpret_cast<const float4*>(sm.a + kk * kPitch + ((4 * ty) ^ sw));
+      const float4 y = *reinterpret_cast<const float4*>(sm.b + kk * kPitch + ((4 * tx) ^ sw));
+      const float xa[4] = {x.x, x.y, x.z, x.w}, yb[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[i][j] = fmaf(xa[i], yb[j], c[i][j]);
+    }
+  }
+}
+
+// Logits of a tile -> its rows' maximum and sum (GRAD = false), or g (GRAD = true, vocabulary rows v0 .. v0 + nv).
+template <bool GRAD>
+__global__ void __launch_bounds__(256) k_loss_logits(LossPlan p, LossBuf b, const float* __restrict__ w, int v0, int nv) {
+  __shared__ __align__(16) TileSmem sm;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int n = *b.n, m0 = blockIdx.y * kT, n0 = blockIdx.x * kT;
+  if (m0 >= n) return;
+  float c[4][4];
+  tile_product<true, true>((const float*)b.x, p.hidden, m0, n, w + (size_t)v0 * p.hidden, p.hidden, n0, nv, 0, p.hidden, sm, c);
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int m = m0 + 4 * ty + i;
+    const bool in = m < n;
+    const int label = in ? b.label[m] - v0 : -1;
+    if (GRAD) {
+      const float l = in ? b.lse[m] : 0.f, up = in ? b.up[m] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int v = n0 + 4 * tx + j;
+        if (in && v < nv)
+          ((float*)b.g)[(size_t)m * p.piece + v] = up * (exp2f((c[i][j] - l) * kLog2e) - (v == label ? 1.f : 0.f));
+      }
+    } else {
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int v = n0 + 4 * tx + j;
+        if (v < nv) top = fmaxf(top, c[i][j]);
+        if (in && v == label) b.picked[m] = c[i][j];
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        // (nothing above -inf: no sum, unless a logit is not a number)
+        if (n0 + 4 * tx + j < nv && !(c[i][j] == -INFINITY)) s += exp2f((c[i][j] - top) * kLog2e);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (in && tx == 0) b.part[(size_t)blockIdx.x * p.rows_pad + m] = make_float2(top, s);
+    }
+  }
+}
+
+// dx sums of a piece: rows x hidden, over the piece's vocabulary rows (blockIdx.z: a part of them).
+__global__ void __launch_bounds__(256) k_loss_dx_tile(LossPlan p, LossBuf b, const float* __restrict__ w, int nv, bool add) {
+  __shared__ __align__(16) TileSmem sm;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int n = *b.n, m0 = blockIdx.y * kT, n0 = blockIdx.x * kT;
+  if (m0 >= n) return;
+  const int per = ((nv + p.splits - 1) / p.splits + 31) / 32 * 32, k0 = min(nv, per * (int)blockIdx.z), k1 = min(nv, k0 + per);
+  float c[4][4];
+  tile_product<true, false>((const float*)b.g, p.piece, m0, n, w, p.hidden, n0, p.hidden, k0, k1, sm, c);
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int m = m0 + 4 * ty + i;
+    if (m >= n) continue;
+    float* a = b.acc + ((size_t)blockIdx.z * p.rows_pad + m) * p.hidden + n0 + 4 * tx;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (n0 + 4 * tx + j < p.hidden) a[j] = add ? a[j] + c[i][j] : c[i][j];
+  }
+}
+
+// dW of a piece: its vocabulary rows x hidden, over the rows.
+__global__ void __launch_bounds__(256) k_loss_dw_tile(LossPlan p, LossBuf b, float* __restrict__ dw, int nv) {
+  __shared__ __align__(16) TileSmem sm;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int m0 = blockIdx.y * kT, n0 = blockIdx.x * kT;
+  float c[4][4];
+  tile_product<false, false>((const float*)b.g, p.piece, m0, nv, (const float*)b.x, p.hidden, n0, p.hidden, 0, *b.n, sm, c);
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int m = m0 + 4 * ty + i;
+    if (m >= nv) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (n0 + 4 * tx + j < p.hidden) dw[(size_t)m * p.hidden + n0 + 4 * tx + j] = c[i][j];
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+constexpr size_t kPieceBytes = 128u << 20;   // g of a piece
+
+int div_up(int a, int b) { return (a + b - 1) / b; }
+
+LossPlan make_plan(int dtype, int rows, int hidden, int vocab) {
+  LossPlan p;
+  p.tc = dtype == PS_DTYPE_BF16;
+  p.rows = rows; p.hidden = hidden; p.vocab = vocab;
+  const int tile_m = p.tc ? 256 : kT;
+  p.tile_v = p.tc ? 256 : kT;
+  p.rows_pad = div_up(std::max(rows, 1), tile_m) * tile_m;
+  p.tiles = p.tc ? 2 * div_up(vocab, p.tile_v) : div_up(vocab, p.tile_v);   // (the tensor cores' tiles in two halves)
+  // the vocabulary in pieces of equal size, no more of them than keep g within kPieceBytes (1024 rows at least)
+  const size_t per_row = (size_t)p.rows_pad * (p.tc ? 2 : 4);
+  const int most = (int)std::max<size_t>(1024, kPieceBytes / per_row / 256 * 256);
+  const int pieces = div_up(vocab, most);
+  p.piece = div_up(div_up(vocab, pieces), 256) * 256;
+  p.splits = 1;
+  if (!p.tc) {   // enough blocks for dx: its tiles times the parts of a piece
+    const int blocks = div_up(rows, kT) * div_up(hidden, kT);
+    while (p.splits < 16 && blocks * p.splits < 2 * 148 && p.piece / (2 * p.splits) >= 64) p.splits *= 2;
+  }
+  return p;
+}
+
+LossBuf carve(void* ws, const LossPlan& p, bool backward) {
+  Carve c(ws);
+  LossBuf b = {};
+  b.n = c.take<int>(1);
+  b.row_of = c.take<int>(p.rows);
+  b.slot = c.take<int>(p.rows);
+  b.label = c.take<int>(p.rows_pad);
+  b.lse = c.take<float>(p.rows_pad);
+  b.up = c.take<float>(p.rows_pad);
+  const size_t es = p.tc ? 2 : 4;
+  b.x = c.take<char>((size_t)p.rows_pad * p.hidden * es);
+  if (!backward) {
+    b.part = c.take<float2>((size_t)p.tiles * p.rows_pad);
+    b.picked = c.take<float>(p.rows_pad);
+  } else {
+    b.g = c.take<char>((size_t)p.rows_pad * p.piece * es);
+    b.acc = c.take<float>((size_t)p.splits * p.rows_pad * p.hidden);
+  }
+  b.bytes = c.at;
+  return b;
+}
+
+bool sizes_ok(int dtype, int rows, int hidden, int vocab) {
+  return (dtype == PS_DTYPE_F32 || dtype == PS_DTYPE_BF16) && rows >= 0 && rows <= (1 << 20) && hidden >= 8 &&
+         hidden <= 65536 && hidden % 8 == 0 && vocab >= 1 && vocab <= (1 << 20);
+}
+ps_status check(const Err& err, int dtype, int rows, int hidden, int vocab, const void* w, const void* dw) {
+  if (dtype != PS_DTYPE_F32 && dtype != PS_DTYPE_BF16) return err(PS_ERR_INVALID_ARG, "ps_lm_loss: dtype must be 0 or 1");
+  if (rows < 0 || rows > (1 << 20) || vocab < 1 || vocab > (1 << 20) || hidden < 1 || hidden > 65536)
+    return err(PS_ERR_INVALID_ARG, "ps_lm_loss: 0 <= rows <= 2^20, 1 <= vocab <= 2^20, 1 <= hidden <= 65536");
+  if (hidden % 8) return err(PS_ERR_UNSUPPORTED, "ps_lm_loss: hidden must be a multiple of 8");
+  if (!aligned(w, 16) || !aligned(dw, 16)) return err(PS_ERR_UNSUPPORTED, "ps_lm_loss: w and dw must lie on a 16-byte boundary");
+  return PS_OK;
+}
+
+// The rows that count and their compact copy.
+cudaError_t launch_rows(const LossArgs& a, const void* x, size_t ldx, const int* labels, const float* lse_in,
+                        const float* dloss, float* loss, float* lse, cudaStream_t st) {
+  const LossPlan& p = a.p;
+  cudaError_t e = launch_after(k_loss_rows, dim3(1), dim3(1024), 0, st, true, p.rows, p.rows_pad, p.vocab, labels, a.b,
+                               lse_in, dloss, loss, lse);
+  if (e != cudaSuccess) return e;
+  const size_t es = p.tc ? 2 : 4;
+  const bool vec = aligned(x, 16) && ldx * es % 16 == 0;
+  if (p.tc)
+    return launch_after(k_loss_gather<__nv_bfloat16>, dim3(p.rows_pad), dim3(256), 0, st, true, p.hidden, 256,
+                        (const __nv_bfloat16*)x, ldx, a.b, vec);
+  return launch_after(k_loss_gather<float>, dim3(p.rows_pad), dim3(256), 0, st, true, p.hidden, kT, (const float*)x, ldx, a.b, vec);
+}
+
+cudaError_t piece_fp32(const LossArgs& a, int v0, int nv, cudaStream_t st) {
+  const LossPlan& p = a.p;
+  const float* w = (const float*)a.w + (size_t)v0 * p.hidden;
+  const unsigned mt = div_up(p.rows, kT), ht = div_up(p.hidden, kT), vt = div_up(nv, kT);
+  cudaError_t e = launch_after(k_loss_logits<true>, dim3(vt, mt), dim3(256), 0, st, true, p, a.b, (const float*)a.w, v0, nv);
+  if (e == cudaSuccess && a.want_dx)
+    e = launch_after(k_loss_dx_tile, dim3(ht, mt, p.splits), dim3(256), 0, st, true, p, a.b, w, nv, v0 > 0);
+  if (e == cudaSuccess && a.dw)
+    e = launch_after(k_loss_dw_tile, dim3(ht, vt), dim3(256), 0, st, true, p, a.b, (float*)a.dw + (size_t)v0 * p.hidden, nv);
+  return e;
+}
+
+}  // namespace
+}  // namespace train
+}  // namespace ps
+
+using namespace ps;
+using namespace ps::train;
+
+extern "C" size_t ps_lm_loss_workspace_bytes(int dtype, int rows, int hidden, int vocab, int backward) {
+  if (!sizes_ok(dtype, rows, hidden, vocab)) return 0;
+  return carve(nullptr, make_plan(dtype, rows, hidden, vocab), backward != 0).bytes;
+}
+
+extern "C" ps_status ps_lm_loss(int dtype, int rows, int hidden, int vocab, const void* x, size_t ldx, const void* w,
+                                const int* labels, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                                int* status, char* err_text, size_t err_cap, void* stream) {
+  const Err err{err_text, err_cap};
+  if (err_text && err_cap) err_text[0] = 0;
+  if (ps_status s = check(err, dtype, rows, hidden, vocab, w, nullptr)) return s;
+  if (rows == 0) return PS_OK;
+  if (!x || !w || !labels || !loss || !lse) return err(PS_ERR_INVALID_ARG, "ps_lm_loss: null pointer");
+  if (ldx < (size_t)hidden) return err(PS_ERR_INVALID_ARG, "ps_lm_loss: ldx is smaller than hidden");
+  LossArgs a = {};
+  a.p = make_plan(dtype, rows, hidden, vocab);
+  a.b = carve(workspace, a.p, false);
+  if (ps_status s = check_workspace(err, "ps_lm_loss", workspace, workspace_bytes, a.b.bytes)) return s;
+  a.w = w;
+  a.status = status ? status : (int*)workspace;
+  cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e = launch_rows(a, x, ldx, labels, nullptr, nullptr, loss, lse, st);
+  if (e == cudaSuccess) {
+    if (a.p.tc) e = loss_forward_tc(a, st);
+    else
+      e = launch_after(k_loss_logits<false>, dim3(a.p.tiles, div_up(rows, kT)), dim3(256), 0, st, true, a.p, a.b, (const float*)w, 0, vocab);
+  }
+  if (e == cudaSuccess)
+    e = launch_after(k_loss_join, dim3(div_up(rows, 8)), dim3(256), 0, st, true, a.p.rows_pad, a.p.tiles, a.b, loss, lse);
+  return err.cuda(e, "ps_lm_loss");
+}
+
+extern "C" ps_status ps_lm_loss_backward(int dtype, int rows, int hidden, int vocab, const void* x, size_t ldx,
+                                         const void* w, const int* labels, const float* lse, const float* dloss, void* dx,
+                                         size_t lddx, void* dw, void* workspace, size_t workspace_bytes, int* status,
+                                         char* err_text, size_t err_cap, void* stream) {
+  const Err err{err_text, err_cap};
+  if (err_text && err_cap) err_text[0] = 0;
+  if (ps_status s = check(err, dtype, rows, hidden, vocab, w, dw)) return s;
+  if (!dx && !dw) return PS_OK;
+  cudaStream_t st = (cudaStream_t)stream;
+  const size_t es = dtype == PS_DTYPE_F32 ? 4 : 2;
+  if (rows == 0) {
+    if (!dw) return PS_OK;
+    return err.cuda(cudaMemsetAsync(dw, 0, (size_t)vocab * hidden * es, st), "ps_lm_loss_backward");
+  }
+  if (!x || !w || !labels || !lse || !dloss) return err(PS_ERR_INVALID_ARG, "ps_lm_loss_backward: null pointer");
+  if (ldx < (size_t)hidden || (dx && lddx < (size_t)hidden))
+    return err(PS_ERR_INVALID_ARG, "ps_lm_loss_backward: ldx or lddx is smaller than hidden");
+  LossArgs a = {};
+  a.p = make_plan(dtype, rows, hidden, vocab);
+  a.b = carve(workspace, a.p, true);
+  if (ps_status s = check_workspace(err, "ps_lm_loss_backward", workspace, workspace_bytes, a.b.bytes)) return s;
+  a.w = w; a.dw = dw; a.want_dx = dx != nullptr;
+  a.status = status ? status : (int*)workspace;
+  cudaError_t e = launch_rows(a, x, ldx, labels, lse, dloss, nullptr, nullptr, st);
+  for (int v0 = 0; e == cudaSuccess && v0 < vocab; v0 += a.p.piece) {
+    const int nv = std::min(a.p.piece, vocab - v0);
+    e = a.p.tc ? loss_piece_tc(a, v0, nv, st) : piece_fp32(a, v0, nv, st);
+  }
+  if (e == cudaSuccess && dx) {
+    const size_t layer = (size_t)a.p.rows_pad * hidden;
+    const bool vec = aligned(dx, 16) && lddx * es % 16 == 0;
+    if (a.p.tc)
+      e = launch_after(k_loss_dx<__nv_bfloat16>, dim3(rows), dim3(256), 0, st, true, hidden, a.p.splits, layer, a.b,
+                       (__nv_bfloat16*)dx, lddx, vec);
+    else
+      e = launch_after(k_loss_dx<float>, dim3(rows), dim3(256), 0, st, true, hidden, a.p.splits, layer, a.b, (float*)dx, lddx, vec);
+  }
+  return err.cuda(e, "ps_lm_loss_backward");
+}
