@@ -1,5 +1,6 @@
 // Attention under the mask of parallel groups (ps_group_attn, ps_group_attn_backward) on the FMA units: every type,
-// stride and alignment.  fp32 runs on these kernels.
+// stride and alignment.  fp32 runs on these kernels; bf16 on the tensor cores' (group_attn_tc.cu) where pointers and strides
+// are multiples of 16 bytes.
 //
 // 64 query rows x 64 keys a step, 256 threads with 4 x 4 scores each; operands widened to fp32 in shared memory,
 // statistics and sums in fp32.  Query tiles hold whole groups, so that the keys of the third kind (a row's own group's
@@ -10,7 +11,7 @@
 //            share the head: its sums need no other block
 // An operand that a row does not see takes no part in its sums (not even times a probability of zero, which
 // would carry a value that is not finite over).
-#include "group_attn.cuh"
+#include "group_attn_tc.cuh"
 
 namespace ps {
 namespace train {
@@ -395,6 +396,12 @@ cudaError_t forward(Seqs s, const AttnArgs& a, cudaStream_t st) {
   return launch_after(k_ga_fwd<T, D>, dim3(tiles, a.n_heads), dim3(kThreads), smem, st, true, s, a);
 }
 template <class T, int D>
+cudaError_t delta_rows(const AttnArgs& a, cudaStream_t st) {
+  if (a.rows == 0) return cudaSuccess;
+  const long long units = (long long)a.rows * a.n_heads;
+  return launch_after(k_ga_delta<T, D>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, true, a);
+}
+template <class T, int D>
 cudaError_t backward(Seqs s, const AttnArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done_q{0}, done_kv{0};
   constexpr int smem_q = smem_tiles<D>(4, 1), smem_kv = smem_tiles<D>(4, 2);
@@ -402,8 +409,7 @@ cudaError_t backward(Seqs s, const AttnArgs& a, cudaStream_t st) {
   if (cudaError_t e = allow_smem((const void*)k_ga_dkv<T, D>, smem_kv, done_kv)) return e;
   cudaError_t e = cudaSuccess;
   if (a.rows > 0) {
-    const long long units = (long long)a.rows * a.n_heads;
-    e = launch_after(k_ga_delta<T, D>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, true, a);
+    e = delta_rows<T, D>(a, st);
     if (e != cudaSuccess) return e;
     const int tiles = number_tiles(s, [&](int, int g) { return div_up(g, groups_per_tile(kT, s.R)); });
     e = launch_after(k_ga_dq<T, D>, dim3(tiles, a.n_heads), dim3(kThreads), smem_q, st, true, s, a);
@@ -435,16 +441,22 @@ ps_status check_sizes(const Err& err, const ps_group_attn_args* a, Seqs* s) {
     s->kv0[b] = (int)kv;
     q += (long long)a->n_groups[b] * s->R;
     kv += a->n_ctx[b] + (long long)a->n_groups[b] * s->R;
-    if (kv >= (1ll << 30)) return err(PS_ERR_INVALID_ARG, "ps_group_attn: 2^30 rows or more");
+    if (kv * a->n_heads >= (1ll << 31)) return err(PS_ERR_INVALID_ARG, "ps_group_attn: rows times n_heads must be below 2^31");
   }
   s->q0[a->B] = (int)q;
   s->kv0[a->B] = (int)kv;
   return PS_OK;
 }
 
-size_t carve(void* ws, const Seqs& s, const ps_group_attn_args* a, bool backward, AttnArgs* g) {
+size_t carve(void* ws, const Seqs& s, const ps_group_attn_args* a, bool backward, AttnArgs* g, TcArgs* t) {
   Carve c(ws);
-  if (backward) g->delta = c.take<float>((size_t)s.q0[s.B] * a->n_heads);
+  const size_t units = (size_t)s.q0[s.B] * a->n_heads;
+  if (backward) g->delta = c.take<float>(units);
+  t->splits = a->dtype == PS_DTYPE_BF16 ? attn_splits(s, a->n_heads, backward) : 1;
+  if (t->splits > 1) {
+    t->part_o = c.take<float>(units * t->splits * a->head_dim);
+    t->part_l = c.take<float>(units * t->splits);
+  }
   return c.at;
 }
 
@@ -465,7 +477,8 @@ ps_status run(const ps_group_attn_args* a, bool backward, void* workspace, size_
       return err(PS_ERR_INVALID_ARG, "ps_group_attn_backward: null pointer");
   }
   AttnArgs g = {};
-  const size_t need = carve(workspace, s, a, backward, &g);
+  TcArgs tc = {};
+  const size_t need = carve(workspace, s, a, backward, &g, &tc);
   if (ps_status e = check_workspace(err, "ps_group_attn", workspace, workspace_bytes, need)) return e;
   if (keys == 0 || (!backward && rows == 0)) return PS_OK;
   g.n_heads = a->n_heads; g.n_kv = a->n_kv_heads; g.per = a->n_heads / a->n_kv_heads;
@@ -477,7 +490,10 @@ ps_status run(const ps_group_attn_args* a, bool backward, void* workspace, size_
   g.status = status ? status : (int*)workspace;
   const bool f32 = a->dtype == PS_DTYPE_F32, d64 = a->head_dim == 64;
   cudaError_t e;
-  if (backward)
+  if (!f32 && attn_tc_takes(g, backward)) {
+    e = backward ? (d64 ? delta_rows<__nv_bfloat16, 64>(g, st) : delta_rows<__nv_bfloat16, 128>(g, st)) : cudaSuccess;
+    if (e == cudaSuccess) e = attn_tc(a->head_dim, backward, s, g, tc, st);
+  } else if (backward)
     e = f32 ? (d64 ? train::backward<float, 64>(s, g, st) : train::backward<float, 128>(s, g, st))
             : (d64 ? train::backward<__nv_bfloat16, 64>(s, g, st) : train::backward<__nv_bfloat16, 128>(s, g, st));
   else
@@ -496,8 +512,9 @@ using namespace ps::train;
 extern "C" size_t ps_group_attn_workspace_bytes(const ps_group_attn_args* a, int backward) {
   Seqs s;
   AttnArgs g = {};
+  TcArgs t = {};
   if (check_sizes(Err{nullptr, 0}, a, &s) != PS_OK) return 0;
-  return carve(nullptr, s, a, backward != 0, &g);
+  return carve(nullptr, s, a, backward != 0, &g, &t);
 }
 extern "C" ps_status ps_group_attn(const ps_group_attn_args* a, void* workspace, size_t workspace_bytes, int* status,
                                    char* err_text, size_t err_cap, void* stream) {

@@ -1,5 +1,5 @@
 // Tensor maps of row-major bf16 matrices for tiled TMA.
-#include "ps_internal.cuh"
+#include "group_attn_tc.cuh"
 
 namespace ps {
 namespace {
@@ -46,4 +46,27 @@ bool make_halves_map(CUtensorMap* m, const void* base, size_t rows, int box_rows
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+namespace train {
+
+bool make_rows_map(CUtensorMap* m, const void* base, size_t rows, size_t cols, size_t ld, int R) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn || rows < (size_t)R) return fn && rows == 0;   // (no rows: nothing asks for the map)
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, 1};
+  cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)R};
+  cuuint32_t box[3] = {(cuuint32_t)kMapCols, 128, 1};
+  cuuint32_t es[3] = {1, 1, 1};
+  if (R > 1) {
+    // Groups may begin at any row: a box starts at (row % R, row / R).  Whole multiples of R rows are described; the
+    // real row of the last group lies among them, since its masks follow it.
+    dims[1] = R;
+    dims[2] = rows / R;
+    box[1] = 1;
+    box[2] = 128;
+  }
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, R > 1 ? 3 : 2, const_cast<void*>(base), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace train
 }  // namespace ps
