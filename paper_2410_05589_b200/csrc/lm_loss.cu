@@ -3,7 +3,7 @@
 //   s = x W^T,  lse = log sum_v exp s_v,  loss = lse - s_label
 //   g = dloss (exp(s - lse) - onehot),    dx = g W,  dW = g^T x
 // Forward: each tile of the product x W^T leaves, per row, the maximum of its logits and the sum of their
-// exponentials against it (and the label's logit where it holds it); a small kernel joins the tiles.  Backward:
+// exponentials against it; a small kernel joins the tiles.  Backward:
 // the logits of a piece of the vocabulary are formed again, turned into g by the epilogue of the product
 // that forms them and kept for the two products that use them.  dx is summed over the pieces in single
 // precision, dW of a piece is complete.
@@ -68,9 +68,13 @@ __global__ void __launch_bounds__(1024) k_loss_rows(int rows, int rows_pad, int 
   }
 }
 
-// Compact copy of the rows that count, zeros up to the end of the last tile.  A block per row.
+// Compact copy of the rows that count, zeros up to the end of the last tile.  A block per row.  Forward (with w) it also
+// forms the label's logit: the products of the tensor cores truncate as they add (a logit of 1.4 over 5120 terms comes out 1e-5
+// too near zero), which a loss would keep in full while its lse averages it.
 template <class T>
-__global__ void __launch_bounds__(256) k_loss_gather(int H, int tile, const T* __restrict__ x, size_t ldx, LossBuf b, bool vec) {
+__global__ void __launch_bounds__(256) k_loss_gather(int H, int tile, const T* __restrict__ x, size_t ldx, const T* __restrict__ w,
+                                                     LossBuf b, bool vec) {
+  __shared__ float s_sum[8];
   pdl_launch_dependents();
   pdl_wait();
   const int n = *b.n, i = blockIdx.x;
@@ -82,10 +86,33 @@ __global__ void __launch_bounds__(256) k_loss_gather(int H, int tile, const T* _
     return;
   }
   const T* src = x + (size_t)b.row_of[i] * ldx;
-  if (vec) {
-    for (int c = threadIdx.x; c < H / N; c += 256) dst[c] = reinterpret_cast<const uint4*>(src)[c];
-  } else {
-    for (int c = threadIdx.x; c < H; c += 256) ((T*)b.x)[(size_t)i * H + c] = src[c];
+  const uint4* row = w ? reinterpret_cast<const uint4*>(w + (size_t)b.label[i] * H) : nullptr;
+  float sum = 0.f;
+  for (int c = threadIdx.x; c < H / N; c += 256) {
+    uint4 v;
+    if (vec) {
+      v = reinterpret_cast<const uint4*>(src)[c];
+    } else {
+      T* e = reinterpret_cast<T*>(&v);
+#pragma unroll
+      for (int j = 0; j < N; ++j) e[j] = src[c * N + j];
+    }
+    dst[c] = v;
+    if (row) {
+      const uint4 u = row[c];
+      const T *e = reinterpret_cast<const T*>(&v), *f = reinterpret_cast<const T*>(&u);
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum = fmaf((float)e[j], (float)f[j], sum);
+    }
+  }
+  if (!row) return;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int k = 1; k < 8; ++k) sum += s_sum[k];
+    b.picked[i] = sum;
   }
 }
 
@@ -241,8 +268,8 @@ __global__ void __launch_bounds__(256) k_loss_logits(LossPlan p, LossBuf b, cons
   for (int i = 0; i < 4; ++i) {
     const int m = m0 + 4 * ty + i;
     const bool in = m < n;
-    const int label = in ? b.label[m] - v0 : -1;
     if (GRAD) {
+      const int label = in ? b.label[m] - v0 : -1;
       const float l = in ? b.lse[m] : 0.f, up = in ? b.up[m] : 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -256,7 +283,6 @@ __global__ void __launch_bounds__(256) k_loss_logits(LossPlan p, LossBuf b, cons
       for (int j = 0; j < 4; ++j) {
         const int v = n0 + 4 * tx + j;
         if (v < nv) top = fmaxf(top, c[i][j]);
-        if (in && v == label) b.picked[m] = c[i][j];
       }
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -385,8 +411,9 @@ cudaError_t launch_rows(const LossArgs& a, const void* x, size_t ldx, const int*
   const bool vec = aligned(x, 16) && ldx * es % 16 == 0;
   if (p.tc)
     return launch_after(k_loss_gather<__nv_bfloat16>, dim3(p.rows_pad), dim3(256), 0, st, true, p.hidden, 256,
-                        (const __nv_bfloat16*)x, ldx, a.b, vec);
-  return launch_after(k_loss_gather<float>, dim3(p.rows_pad), dim3(256), 0, st, true, p.hidden, kT, (const float*)x, ldx, a.b, vec);
+                        (const __nv_bfloat16*)x, ldx, (const __nv_bfloat16*)(loss ? a.w : nullptr), a.b, vec);
+  return launch_after(k_loss_gather<float>, dim3(p.rows_pad), dim3(256), 0, st, true, p.hidden, kT, (const float*)x, ldx,
+                      (const float*)(loss ? a.w : nullptr), a.b, vec);
 }
 
 cudaError_t piece_fp32(const LossArgs& a, int v0, int nv, cudaStream_t st) {

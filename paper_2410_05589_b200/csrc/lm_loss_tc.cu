@@ -1,6 +1,6 @@
 // Products of the LM-head loss on the 5th-generation tensor cores (bf16 operands, fp32 sums):
 //
-//   forward   S = X W^T  -> per row and half tile: maximum, sum of exponentials, the label's logit
+//   forward   S = X W^T  -> per row and half tile: maximum, sum of exponentials
 //   gradient  S = X W^T  -> G = up (exp(S - lse) - onehot), rounded to bf16 (the operand type of the two products
 //                           that read it; what they add up is fp32)
 //   dx        G W        -> sums over the pieces in fp32
@@ -230,7 +230,6 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
       const int m = mt * kTile + (int)rank * 128 + r, c0 = nt * kTile + half * 128;
       const uint32_t ta = tmem + ((uint32_t)(32 * q) << 16) + buf * kTile + half * 128;
       if (MODE == FWD) {
-        const int label = a.b.label[m];
         float top = -INFINITY, sum = 0.f;
 #pragma unroll 1
         for (int j0 = 0; j0 < 128; j0 += 32) {
@@ -242,11 +241,6 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
           for (int j = 0; j < 32; ++j) {
             if (j >= left) v[j] = -INFINITY;
             mx = fmaxf(mx, v[j]);
-          }
-          if ((unsigned)(label - c0 - j0) < 32u) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (label - c0 - j0 == j) a.b.picked[m] = v[j];
           }
           const float l = mx > -INFINITY ? mx * kLog2e : 0.f;   // (nothing above -inf: the sum stays 0, or no number)
           sum *= top > -INFINITY ? exp2f(top * kLog2e - l) : 0.f;
