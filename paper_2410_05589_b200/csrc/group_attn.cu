@@ -448,15 +448,22 @@ ps_status check_sizes(const Err& err, const ps_group_attn_args* a, Seqs* s) {
   return PS_OK;
 }
 
-size_t carve(void* ws, const Seqs& s, const ps_group_attn_args* a, bool backward, AttnArgs* g, TcArgs* t) {
+size_t carve(void* ws, const Seqs& s, const ps_group_attn_args* a, bool backward, AttnArgs* g, TcArgs* t, TcArgs* tk) {
   Carve c(ws);
   const size_t units = (size_t)s.q0[s.B] * a->n_heads;
   if (backward) g->delta = c.take<float>(units);
-  t->splits = a->dtype == PS_DTYPE_BF16 ? attn_splits(s, a->n_heads, backward) : 1;
-  if (t->splits > 1) {
-    t->part_o = c.take<float>(units * t->splits * a->head_dim);
-    t->part_l = c.take<float>(units * t->splits);
+  if (a->dtype != PS_DTYPE_BF16) return c.at;
+  t->gpt = tk->gpt = groups_per_tile(128, s.R);
+  t->splits = attn_splits(s, a->n_heads, backward);
+  const size_t parts_q = t->splits > 1 ? units * t->splits * a->head_dim : 0;
+  size_t parts_k = 0;
+  if (backward) {
+    attn_parts(s, a->n_kv_heads, a->n_heads / a->n_kv_heads, tk);
+    if (tk->parts > 1) parts_k = (size_t)tk->key_units * 2 * 128 * a->head_dim;
   }
+  // (dq's parts are joined before dk and dv are formed)
+  t->part_o = tk->part_o = c.take<float>(std::max(parts_q, parts_k));
+  t->part_l = c.take<float>(t->splits > 1 && !backward ? units * t->splits : 0);
   return c.at;
 }
 
@@ -477,8 +484,8 @@ ps_status run(const ps_group_attn_args* a, bool backward, void* workspace, size_
       return err(PS_ERR_INVALID_ARG, "ps_group_attn_backward: null pointer");
   }
   AttnArgs g = {};
-  TcArgs tc = {};
-  const size_t need = carve(workspace, s, a, backward, &g, &tc);
+  TcArgs tc = {}, tk = {};
+  const size_t need = carve(workspace, s, a, backward, &g, &tc, &tk);
   if (ps_status e = check_workspace(err, "ps_group_attn", workspace, workspace_bytes, need)) return e;
   if (keys == 0 || (!backward && rows == 0)) return PS_OK;
   g.n_heads = a->n_heads; g.n_kv = a->n_kv_heads; g.per = a->n_heads / a->n_kv_heads;
@@ -490,10 +497,9 @@ ps_status run(const ps_group_attn_args* a, bool backward, void* workspace, size_
   g.status = status ? status : (int*)workspace;
   const bool f32 = a->dtype == PS_DTYPE_F32, d64 = a->head_dim == 64;
   cudaError_t e;
-  if (!f32 && attn_tc_takes(g, backward)) {
-    e = backward ? (d64 ? delta_rows<__nv_bfloat16, 64>(g, st) : delta_rows<__nv_bfloat16, 128>(g, st)) : cudaSuccess;
-    if (e == cudaSuccess) e = attn_tc(a->head_dim, backward, s, g, tc, st);
-  } else if (backward)
+  if (!f32 && attn_tc_takes(g, backward))
+    e = attn_tc(a->head_dim, backward, s, g, tc, tk, st);
+  else if (backward)
     e = f32 ? (d64 ? train::backward<float, 64>(s, g, st) : train::backward<float, 128>(s, g, st))
             : (d64 ? train::backward<__nv_bfloat16, 64>(s, g, st) : train::backward<__nv_bfloat16, 128>(s, g, st));
   else
@@ -512,9 +518,9 @@ using namespace ps::train;
 extern "C" size_t ps_group_attn_workspace_bytes(const ps_group_attn_args* a, int backward) {
   Seqs s;
   AttnArgs g = {};
-  TcArgs t = {};
+  TcArgs t = {}, tk = {};
   if (check_sizes(Err{nullptr, 0}, a, &s) != PS_OK) return 0;
-  return carve(nullptr, s, a, backward != 0, &g, &t);
+  return carve(nullptr, s, a, backward != 0, &g, &t, &tk);
 }
 extern "C" ps_status ps_group_attn(const ps_group_attn_args* a, void* workspace, size_t workspace_bytes, int* status,
                                    char* err_text, size_t err_cap, void* stream) {

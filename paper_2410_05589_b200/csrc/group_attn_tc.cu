@@ -3,7 +3,7 @@
 //
 //   forward  S = Q K^T,  P = exp(S - max),  O += P V                 query rows on the 128 lanes
 //   dq       S = Q K^T,  dP = dO V^T,  dQ += dS K                    query rows on the lanes
-//   dk, dv   S^T = K Q^T,  dP^T = V dO^T,  dV += P^T dO,  dK += dS^T Q   keys on the lanes
+//   dk, dv   S^T = K Q^T,  dP^T = V dO^T,  dV += P^T dO,  dK += dS^T Q   keys on the lanes (masks: see k_gat_masks)
 // with dS = P (dP - delta).  P and dS are rounded to bf16, the operand type of the products that read them (the sums are
 // fp32); they go from registers to tensor memory and are read there as the products' A operand, so that
 // shared memory holds nothing but Q, K, V and dO, which tiled TMA brings in the one layout (rows of 64 values,
@@ -95,67 +95,144 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float m;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
+  return m;
+}
+// Two fp32 operations an instruction.
+struct f2 { float x, y; };
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 d;
+  asm("{\n\t.reg .b64 p, q, r, s;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmov.b64 r, {%6, %7};\n\t"
+      "fma.rn.f32x2 s, p, q, r;\n\tmov.b64 {%0, %1}, s;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 d;
+  asm("{\n\t.reg .b64 p, q, s;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\t"
+      "add.rn.f32x2 s, p, q;\n\tmov.b64 {%0, %1}, s;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 d;
+  asm("{\n\t.reg .b64 p, q, s;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\t"
+      "mul.rn.f32x2 s, p, q;\n\tmov.b64 {%0, %1}, s;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ f2 pair_of(const uint32_t* v) { return f2{__uint_as_float(v[0]), __uint_as_float(v[1])}; }
 __device__ __forceinline__ bool all_sync(bool p) { return __all_sync(0xffffffffu, p); }
 
 // Operands in shared memory: a tile is D / 64 halves of 128 rows of 128 bytes (swizzled), 8 rows 1024 bytes.  K-major
-// (products over head_dim): step ks of 16 columns.  MN-major (products over rows): step ks of 16 rows.
-__device__ __forceinline__ uint64_t desc_k(uint32_t s, int ks) {
-  const uint32_t at = s + (ks >> 2) * kHalfBytes + (ks & 3) * 32;
-  return (uint64_t)((at & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+// (products over head_dim) or MN-major (products over rows: 64 columns, then the other half); what a step of 16 columns or 16
+// rows adds is a constant, since the issuing thread's instructions between two products are time the tensor cores wait.
+__device__ __forceinline__ uint64_t desc_k(uint32_t s) {
+  return (uint64_t)((s & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
-__device__ __forceinline__ uint64_t desc_mn(uint32_t s, int ks) {
-  const uint32_t at = s + ks * 2048;
-  return (uint64_t)((at & 0x3FFFFu) >> 4) | ((uint64_t)(kHalfBytes >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+__device__ __forceinline__ uint64_t desc_mn(uint32_t s) {
+  return (uint64_t)((s & 0x3FFFFu) >> 4) | ((uint64_t)(kHalfBytes >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
          ((uint64_t)2 << 61);
 }
+__host__ __device__ constexpr int step_k(int ks) { return ((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4; }
+__host__ __device__ constexpr int step_mn(int ks) { return ks * 2048 >> 4; }
 // fp32 sums, bf16 operands, 128 lanes, n columns; the B operand MN-major or not.
 __device__ __forceinline__ constexpr uint32_t idesc(int n, bool b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
 // d = A B^T over head_dim, both operands from shared memory.
 template <int D>
-__device__ __forceinline__ void mma_scores(uint32_t d, uint32_t a, uint32_t b) {
+__device__ __forceinline__ void mma_scores(uint32_t d, uint64_t a, uint64_t b) {
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) umma::mma_f16(d, desc_k(a, ks), desc_k(b, ks), idesc(kT, false), ks > 0);
+  for (int ks = 0; ks < D / 16; ++ks) umma::mma_f16(d, a + step_k(ks), b + step_k(ks), idesc(kT, false), ks > 0);
 }
 // d (+)= A B over 128 rows, A (bf16) in tensor memory: its columns 0..63 and 64..127 at `half` columns' distance.
 template <int D>
-__device__ __forceinline__ void mma_sums(uint32_t d, uint32_t a, int half, uint32_t b, bool add) {
+__device__ __forceinline__ void mma_sums(uint32_t d, uint32_t a, int half, uint64_t b, bool add) {
 #pragma unroll
   for (int ks = 0; ks < kT / 16; ++ks)
-    mma_ts(d, a + (ks >> 2) * half + (ks & 3) * 8, desc_mn(b, ks), idesc(D, true), add || ks > 0);
+    mma_ts(d, a + (ks >> 2) * half + (ks & 3) * 8, b + step_mn(ks), idesc(D, true), add || ks > 0);
 }
 
 // ---- tiles ------------------------------------------------------------------------------------------
-// A query tile's walk over the key tiles.
+// Key tiles that one or two query tiles of a sequence go through, in order: the context, the real rows up to those
+// of the last group, then (R > 1) each query tile's own rows.
 struct KeyWalk {
-  int ctx, R, n_real, rows, rho0;
-  int n_ctx, n_rt, total;
+  int ctx, R, n_real;              // n_real: groups up to the last of the query tiles
+  int n_ctx, n_shared, total;
   int kv0, g0;                     // first context row, first group row of the sequence
-  __device__ KeyWalk(const Seqs& s, int b, int rho0_, int rows_) {
-    ctx = s.ctx[b]; R = s.R; rho0 = rho0_; rows = rows_;
+  __device__ void start(const Seqs& s, int b, int group_end) {
+    ctx = s.ctx[b]; R = s.R; n_real = group_end;
     kv0 = s.kv0[b];
     g0 = kv0 + ctx;
-    n_real = (rho0 + rows - 1) / R + 1;
     n_ctx = div_up(ctx, kT);
-    n_rt = div_up(n_real, kT);
-    total = n_ctx + n_rt + (R > 1);
+    n_shared = n_ctx + div_up(n_real, kT);
+    total = n_shared + (R > 1);
   }
-  // Kind of tile i, its first key's index among those of its kind and their number.
-  __device__ int tile(int i, int& x0, int& n) const {
+  // Kind of tile i, its first key's index among those of its kind and their number; for the query tile whose first
+  // group is `group` and that has n_rows.
+  __device__ int tile(int i, int group, int n_rows, int& x0, int& n) const {
     if (i < n_ctx) { x0 = i * kT; n = min(kT, ctx - x0); return CTX; }
-    if (i < n_ctx + n_rt) { x0 = (i - n_ctx) * kT; n = min(kT, n_real - x0); return REAL; }
-    x0 = rho0; n = rows; return LOCAL;
+    if (i < n_shared) { x0 = (i - n_ctx) * kT; n = min(kT, n_real - x0); return REAL; }
+    x0 = group * R; n = n_rows; return LOCAL;
   }
   __device__ int key_row(int kind, int x) const { return kind == CTX ? kv0 + x : (kind == REAL ? g0 + x * R : g0 + x); }
-  // Columns that query row r of the tile sees (rows that only fill the tile up: all of them).
-  __device__ void sees(int kind, int x0, int n, int r, int& lo, int& hi) const {
+};
+// Row r of a query tile: its group within the tile and its place in the group.
+struct TileRow {
+  int r, group, place;
+  __device__ TileRow(int r_, int R) : r(r_), group(r_ / R), place(r_ - r_ / R * R) {}
+  // Columns of a key tile that it sees (rows that only fill the query tile up: all of them).
+  __device__ void sees(int kind, int x0, int n, int first_group, int n_rows, int& lo, int& hi) const {
     lo = 0;
     hi = n - 1;
-    if (r >= rows) return;
-    if (kind == REAL) hi = min(hi, (rho0 + r) / R - x0);
-    if (kind == LOCAL) { lo = r - r % R + 1; hi = r; }
+    if (r >= n_rows) return;
+    if (kind == REAL) hi = min(hi, first_group + group - x0);
+    if (kind == LOCAL) { lo = r - place + 1; hi = r; }
   }
+};
+
+// One unit of work of the kernels whose lanes are query rows: up to NT neighbouring query tiles of a head and a
+// part of their key tiles.  (It goes by value, and its two tiles' fields by selection, to stay in registers: as an object in
+// memory it was read again behind every instruction that may touch memory.)
+template <int NT>
+struct QueryWork {
+  int b, h, split, nt, group0, group1, rows0, rows1, qrow0, i0, i1, gpt;
+  KeyWalk w;
+  __device__ static int count(const Seqs& s, const AttnArgs& a, const TcArgs& t) { return s.tile0[s.B] * a.n_heads * t.splits; }
+  // (unit 0 is the last one: the longest rows of the longest sequence)
+  __device__ QueryWork(const Seqs& s, const AttnArgs& a, const TcArgs& t, int unit) {
+    int u = count(s, a, t) - 1 - unit;
+    split = 0;
+    if (t.splits > 1) { split = u % t.splits; u /= t.splits; }
+    const int tile = u / a.n_heads;
+    gpt = t.gpt;
+    h = u - tile * a.n_heads;
+    b = seq_of_tile(s, tile);
+    group0 = (tile - s.tile0[b]) * NT * gpt;
+    group1 = group0 + gpt;
+    const int left = s.groups[b] - group0;
+    rows0 = min(gpt, left) * s.R;
+    rows1 = NT == 1 ? 0 : max(0, min(gpt, left - gpt)) * s.R;
+    nt = rows1 > 0 ? 2 : 1;
+    qrow0 = s.q0[b] + group0 * s.R;
+    w.start(s, b, group0 + min(NT * gpt, left));
+    i0 = 0;
+    i1 = w.total;
+    if (t.splits > 1) {
+      i0 = w.total * split / t.splits;
+      i1 = w.total * (split + 1) / t.splits;
+    }
+  }
+  // Of query tile x: first group, rows, first row.
+  __device__ int group(int x) const { return x ? group1 : group0; }
+  __device__ int rows(int x) const { return x ? rows1 : rows0; }
+  __device__ int qrow(int x) const { return qrow0 + x * gpt * w.R; }
 };
 
 // 128 rows of K or V (columns col ..) to shared memory.
@@ -220,41 +297,43 @@ __device__ __forceinline__ void alloc_tmem(uint32_t* where, int cols) {
 }
 
 // ---- forward ----------------------------------------------------------------------------------------
-// Two blocks an SM, each with one query tile: one's softmax runs beside the other's products.  Warp 0 issues the
-// TMA loads, warp 1 the MMAs, warps 2..5 own a row a thread.  S of the next key tile is issued behind O += P V of this
-// one (P lies in S's columns: the tensor cores work in order), K and V pass through a ring.
+// A persistent block an SM; a unit of its work are two neighbouring query tiles of a head, which share the key tiles
+// that pass through the ring.  Warp 0 issues the TMA loads, warp 1 the MMAs, four warps per query tile own a row a
+// thread.  The queue of the tensor cores is O0 += P0 V, S0 of the next keys, O1 += P1 V, S1 of the next keys (P lies in
+// S's columns: they work in order), so that one tile's softmax runs beside the other's products.
 template <int D>
 struct Fwd {
-  static constexpr int NS = D == 128 ? 2 : 4;
-  static constexpr int threads = 192, cols = 256;
-  static constexpr int smem = (1 + NS) * kTileBytes<D> + 2048;
+  static constexpr int NS = D == 128 ? 5 : 10;
+  static constexpr int threads = 320;
+  static constexpr int smem = (2 + NS) * kTileBytes<D> + 2048;
 };
 struct FwdCtl {
-  uint64_t full[4], empty[4], q_full, s_full, p_full, o_full;
+  uint64_t full[10], empty[10], q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_empty[2];
   uint32_t tmem;
   int abort_flag;
 };
 
-// Row r of the tile over the key tiles [i0, i1), by one warp and over the keys it sees alone.
+// Row r of query tile x over its key tiles [i0, i1), by one warp and over the keys it sees alone.
 template <int D>
-__device__ __noinline__ void fwd_row(const Seqs& s, const AttnArgs& a, const TcArgs& t, const KeyWalk& w, int h, int r, int qrow, int i0,
-                                     int i1, int split) {
-  const int lane = threadIdx.x & 31;
+__device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const QueryWork<2> u, int x, int r) {
+  const int lane = threadIdx.x & 31, h = u.h;
+  const size_t row_q = (size_t)u.qrow(x) + r;
+  const TileRow tr(r, u.w.R);
   const bf16 *k = (const bf16*)a.k + (size_t)(h / a.per) * D, *v = (const bf16*)a.v + (size_t)(h / a.per) * D;
   float q[D / 32], o[D / 32], m = -INFINITY, l = 0.f;
-  lane_load<D>((const bf16*)a.q + (size_t)(qrow + r) * a.ldq + (size_t)h * D, lane, q);
+  lane_load<D>((const bf16*)a.q + row_q * a.ldq + (size_t)h * D, lane, q);
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-  for (int i = i0; i < i1; ++i) {
+  for (int i = u.i0; i < u.i1; ++i) {
     int x0, n, lo, hi;
-    const int kind = w.tile(i, x0, n);
-    w.sees(kind, x0, n, r, lo, hi);
+    const int kind = u.w.tile(i, u.group(x), u.rows(x), x0, n);
+    tr.sees(kind, x0, n, u.group(x), u.rows(x), lo, hi);
     for (int c = lo; c <= hi; ++c) {
-      const size_t row = w.key_row(kind, x0 + c);
-      float x[D / 32], y[D / 32];
-      lane_load<D>(k + row * a.ldk, lane, x);
+      const size_t row = u.w.key_row(kind, x0 + c);
+      float kx[D / 32], y[D / 32];
+      lane_load<D>(k + row * a.ldk, lane, kx);
       lane_load<D>(v + row * a.ldv, lane, y);
-      const float sc = lane_dot<D>(q, x) * a.scale;
+      const float sc = lane_dot<D>(q, kx) * a.scale;
       if (sc > m) {
         const float f = m > -INFINITY ? exp2f((m - sc) * kLog2e) : 0.f;
         l *= f;
@@ -270,12 +349,12 @@ __device__ __noinline__ void fwd_row(const Seqs& s, const AttnArgs& a, const TcA
   }
   const float inv = l == 0.f ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : m + logf(l);
   if (t.splits == 1) {
-    bf16* dst = (bf16*)a.out + (size_t)(qrow + r) * a.ldo + (size_t)h * D;
+    bf16* dst = (bf16*)a.out + row_q * a.ldo + (size_t)h * D;
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * inv);
-    if (lane == 0) a.lse[(size_t)h * a.rows + qrow + r] = lse;
+    if (lane == 0) a.lse[(size_t)h * a.rows + row_q] = lse;
   } else {
-    const size_t at = ((size_t)split * a.n_heads + h) * a.rows + qrow + r;
+    const size_t at = ((size_t)u.split * a.n_heads + h) * a.rows + row_q;
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) t.part_o[at * D + lane + 32 * e] = o[e] * inv;
     if (lane == 0) t.part_l[at] = lse;
@@ -283,167 +362,216 @@ __device__ __noinline__ void fwd_row(const Seqs& s, const AttnArgs& a, const TcA
 }
 
 template <int D>
-__global__ void __launch_bounds__(Fwd<D>::threads, 2)
+__global__ void __launch_bounds__(Fwd<D>::threads, 1)
 k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a,
           const __grid_constant__ TcArgs t) {
   using F = Fwd<D>;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t sq = base, ring = base + kTileBytes<D>;
-  FwdCtl& ctl = *reinterpret_cast<FwdCtl*>(smem_raw + (base - raw) + (1 + F::NS) * kTileBytes<D>);
+  const uint32_t sq = base, ring = base + 2 * kTileBytes<D>;
+  FwdCtl& ctl = *reinterpret_cast<FwdCtl*>(smem_raw + (base - raw) + (2 + F::NS) * kTileBytes<D>);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < F::NS; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
-    mbar_init(&ctl.q_full, 1);
-    mbar_init(&ctl.s_full, 1);
-    mbar_init(&ctl.p_full, 4);
-    mbar_init(&ctl.o_full, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&ctl.q_full[i], 1); mbar_init(&ctl.q_empty[i], 1);
+      mbar_init(&ctl.s_full[i], 1); mbar_init(&ctl.p_full[i], 4);
+      mbar_init(&ctl.o_full[i], 1); mbar_init(&ctl.o_empty[i], 4);
+    }
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
   }
   if (warp == 1) {
     __syncwarp();
-    alloc_tmem(&ctl.tmem, F::cols);
+    alloc_tmem(&ctl.tmem, 512);
     fence_before_sync();
   }
   __syncthreads();
   fence_after_sync();
-  const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_o = tmem + kT;
+  const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_o = tmem + 2 * kT;
   volatile int* abort_flag = &ctl.abort_flag;
-  // (the longest rows first, all heads of a tile side by side)
-  const int u = (int)(gridDim.x - 1 - blockIdx.x), tile = u / a.n_heads, h = u - tile * a.n_heads, split = blockIdx.y, b = seq_of_tile(s, tile);
-  const int gpt = groups_per_tile(kT, s.R), g0 = (tile - s.tile0[b]) * gpt, rows = min(gpt, s.groups[b] - g0) * s.R;
-  const KeyWalk w(s, b, g0 * s.R, rows);
-  const int qrow = s.q0[b] + w.rho0, i0 = w.total * split / t.splits, i1 = w.total * (split + 1) / t.splits;
+  const int units = QueryWork<2>::count(s, a, t);
   pdl_wait();
 
   if (warp == 0) {
-    if (lane == 0 && i0 < i1) {
-      load_rows<D>(sq, &maps.q, qrow, h * D, &ctl.q_full);
-      const int col = h / a.per * D;
-      int it = 0;
-      for (int i = i0; i < i1; ++i) {
-        int x0, n;
-        const int kind = w.tile(i, x0, n), row0 = kind == CTX ? w.kv0 : w.g0;
-        for (int kv = 0; kv < 2; ++kv, ++it) {
-          const int slot = it % F::NS;
-          if (!mbar_wait(&ctl.empty[slot], ((it / F::NS) & 1) ^ 1, abort_flag)) { i = i1; break; }
-          load_keys<D>(ring + slot * kTileBytes<D>, kv ? &maps.v : &maps.k, kv ? &maps.vs : &maps.ks, kind, row0, s.R, x0, col,
-                       &ctl.full[slot]);
+    if (lane == 0) {
+      int it = 0, nq[2] = {0, 0};
+      bool ok = true;
+      auto slot_of = [&](uint32_t& dst, uint64_t*& bar) {   // the next slot of the ring, when it is free
+        const int slot = it % F::NS;
+        ok = mbar_wait(&ctl.empty[slot], ((it / F::NS) & 1) ^ 1, abort_flag);
+        dst = ring + slot * kTileBytes<D>;
+        bar = &ctl.full[slot];
+        ++it;
+        return ok;
+      };
+      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+        const QueryWork<2> u(s, a, t, unit);
+        if (u.i0 == u.i1) continue;
+        for (int x = 0; ok && x < u.nt; ++x) {
+          ok = mbar_wait(&ctl.q_empty[x], (nq[x]++ & 1) ^ 1, abort_flag);
+          if (ok) load_rows<D>(sq + x * kTileBytes<D>, &maps.q, u.qrow(x), u.h * D, &ctl.q_full[x]);
+        }
+        const int col = u.h / a.per * D;
+        uint32_t dst;
+        uint64_t* bar;
+        for (int i = u.i0; ok && i < u.i1; ++i) {
+          for (int kv = 0; ok && kv < 2; ++kv)
+            for (int x = 0; ok && x < (i < u.w.n_shared ? 1 : u.nt); ++x) {
+              int x0, n;
+              const int kind = u.w.tile(i, u.group(x), u.rows(x), x0, n), row0 = kind == CTX ? u.w.kv0 : u.w.g0;
+              if (slot_of(dst, bar)) load_keys<D>(dst, kv ? &maps.v : &maps.k, kv ? &maps.vs : &maps.ks, kind, row0, s.R, x0, col, bar);
+            }
         }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && i0 < i1) {
-      const int n = i1 - i0;
-      auto scores = [&](int i) {
-        const int it = 2 * i, slot = it % F::NS;
-        if (!mbar_wait(&ctl.full[slot], (it / F::NS) & 1, abort_flag)) return false;
+    if (lane == 0) {
+      int pos = 0, nq[2] = {0, 0}, np[2] = {0, 0};
+      bool ok = true;
+      auto wait_slot = [&](int it) {
+        ok = ok && mbar_wait(&ctl.full[it % F::NS], (it / F::NS) & 1, abort_flag);
         fence_after_sync();
-        mma_scores<D>(tmem, sq, ring + slot * kTileBytes<D>);
-        mma_commit(&ctl.s_full);
-        mma_commit(&ctl.empty[slot]);
-        return true;
+        return ring + it % F::NS * kTileBytes<D>;
       };
-      bool ok = mbar_wait(&ctl.q_full, 0, abort_flag) && scores(0);
-      for (int i = 0; ok && i < n; ++i) {
-        const int it = 2 * i + 1, slot = it % F::NS;
-        ok = mbar_wait(&ctl.full[slot], (it / F::NS) & 1, abort_flag) && mbar_wait(&ctl.p_full, i & 1, abort_flag);
-        if (!ok) break;
-        fence_after_sync();
-        mma_sums<D>(t_o, tmem, 32, ring + slot * kTileBytes<D>, i > 0);
-        mma_commit(&ctl.empty[slot]);
-        if (i + 1 < n) ok = scores(i + 1);
-        else mma_commit(&ctl.o_full);
+      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+        const QueryWork<2> u(s, a, t, unit);
+        if (u.i0 == u.i1) continue;
+        // S of query tile x with the key tile whose slots begin at `at`
+        auto scores = [&](int i, int at, int x) {
+          const bool own = i >= u.w.n_shared;
+          const uint32_t k = wait_slot(own ? at + x : at);
+          if (!ok) return;
+          mma_scores<D>(tmem + x * kT, desc_k(sq + x * kTileBytes<D>), desc_k(k));
+          mma_commit(&ctl.s_full[x]);
+          if (own || x == u.nt - 1) mma_commit(&ctl.empty[(own ? at + x : at) % F::NS]);
+          if (i == u.i1 - 1) mma_commit(&ctl.q_empty[x]);
+        };
+        for (int x = 0; ok && x < u.nt; ++x) {
+          ok = mbar_wait(&ctl.q_full[x], nq[x] & 1, abort_flag);
+          if (ok) scores(u.i0, pos, x);
+        }
+        for (int i = u.i0; ok && i < u.i1; ++i) {
+          const bool own = i >= u.w.n_shared;
+          const int next = pos + (own ? 2 * u.nt : 2);
+          for (int x = 0; ok && x < u.nt; ++x) {
+            const int vs = own ? pos + u.nt + x : pos + 1;
+            const uint32_t v = wait_slot(vs);
+            ok = ok && mbar_wait(&ctl.p_full[x], np[x]++ & 1, abort_flag);
+            if (ok && i == u.i0) ok = mbar_wait(&ctl.o_empty[x], (nq[x]++ & 1) ^ 1, abort_flag);
+            if (!ok) break;
+            fence_after_sync();
+            mma_sums<D>(t_o + x * kT, tmem + x * kT, 32, desc_mn(v), i > u.i0);
+            if (own || x == u.nt - 1) mma_commit(&ctl.empty[vs % F::NS]);
+            if (i == u.i1 - 1) mma_commit(&ctl.o_full[x]);
+            else scores(i + 1, next, x);
+          }
+          pos = next;
+        }
       }
     }
   } else {
-    const int q = warp & 3, r = 32 * q + lane;
-    const uint32_t lanes = (uint32_t)(32 * q) << 16;
+    const int q = warp & 3, r = 32 * q + lane, x = (warp - 2) >> 2;
+    const uint32_t lanes = (uint32_t)(32 * q) << 16, ts = tmem + x * kT + lanes, to = t_o + x * kT + lanes;
     const float c = a.scale * kLog2e;
-    float m = -INFINITY, l = 0.f;
+    const TileRow tr(r, s.R);
+    int ns = 0, nu = 0;
     bool ok = true;
-    for (int i = i0; i < i1; ++i) {
-      int x0, n, lo, hi;
-      const int kind = w.tile(i, x0, n);
-      w.sees(kind, x0, n, r, lo, hi);
-      ok = all_sync(mbar_wait(&ctl.s_full, (i - i0) & 1, abort_flag));
-      if (!ok) break;
-      fence_after_sync();
-      uint32_t v[kT];
+    for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      const QueryWork<2> u(s, a, t, unit);
+      if (x >= u.nt) continue;
+      const int rows = u.rows(x), group = u.group(x);
+      float m = -INFINITY, l = 0.f;
+      for (int i = u.i0; i < u.i1; ++i, ++ns) {
+        int x0, n, lo, hi;
+        const int kind = u.w.tile(i, group, rows, x0, n);
+        tr.sees(kind, x0, n, group, rows, lo, hi);
+        ok = all_sync(mbar_wait(&ctl.s_full[x], ns & 1, abort_flag));
+        if (!ok) break;
+        fence_after_sync();
+        uint32_t v[kT];
 #pragma unroll
-      for (int j = 0; j < kT; j += 32) ld32(tmem + lanes + j, v + j);
-      ld_wait();
-      if (!all_sync(lo <= 0 && hi >= kT - 1)) {
+        for (int j = 0; j < kT; j += 32) ld32(ts + j, v + j);
+        ld_wait();
+        if (!all_sync(hi >= kT - 1)) {
 #pragma unroll
-        for (int j = 0; j < kT; ++j)
-          if (j < lo || j > hi) v[j] = 0xFF800000u;   // -inf
-      }
-      float x[4] = {m, -INFINITY, -INFINITY, -INFINITY};
+          for (int j = 0; j < kT; ++j)
+            if (j > hi) v[j] = 0xFF800000u;   // -inf
+        }
+        if (!all_sync(lo <= 0)) {
 #pragma unroll
-      for (int j = 0; j < kT; j += 4)
+          for (int j = 0; j < kT; ++j)
+            if (j < lo) v[j] = 0xFF800000u;
+        }
+        float y[4] = {m, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = fmaxf(x[e], __uint_as_float(v[j + e]));
-      const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      if (i == i0) {
-        m = top;
-      } else {
-        // the sums stay relative to an older maximum until one has grown by 2^kSlack (the products so far are
-        // complete: S of this tile was issued behind them)
-        const bool grown = (top - m) * c > kSlack;
-        if (__any_sync(0xffffffffu, grown)) {
-          const float f = grown ? ex2((m - top) * c) : 1.f;
-          l *= f;
-          if (grown) m = top;
+        for (int j = 0; j < kT; j += 8)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = max3(y[e], __uint_as_float(v[j + e]), __uint_as_float(v[j + 4 + e]));
+        const float top = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+        if (i == u.i0) {
+          m = top;
+        } else {
+          // the sums stay relative to an older maximum until one has grown by 2^kSlack (the products so far are
+          // complete: S of this tile was issued behind them)
+          const bool grown = (top - m) * c > kSlack;
+          if (__any_sync(0xffffffffu, grown)) {
+            const float f = grown ? ex2((m - top) * c) : 1.f;
+            l *= f;
+            if (grown) m = top;
 #pragma unroll 1
-          for (int j = 0; j < D; j += 32) {
-            uint32_t o[32];
-            ld32(t_o + lanes + j, o);
-            ld_wait();
+            for (int j = 0; j < D; j += 32) {
+              uint32_t o[32];
+              ld32(to + j, o);
+              ld_wait();
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            st32(t_o + lanes + j, o);
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              st32(to + j, o);
+            }
           }
         }
-      }
-      const float ref = m > -INFINITY ? m * c : 0.f;
-      float sum[2] = {0.f, 0.f};
+        const float ref = m > -INFINITY ? m * c : 0.f;
+        f2 sum = {0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < kT; j += 32) {
-        uint32_t p[16];
+        for (int j = 0; j < kT; j += 32) {
+          uint32_t p[16];
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          const float y0 = ex2(fmaf(__uint_as_float(v[j + e]), c, -ref)), y1 = ex2(fmaf(__uint_as_float(v[j + e + 1]), c, -ref));
-          sum[0] += y0;
-          sum[1] += y1;
-          p[e / 2] = pack2(y0, y1);
+          for (int e = 0; e < 32; e += 2) {
+            const f2 z = fma2(pair_of(v + j + e), f2{c, c}, f2{-ref, -ref}), w = {ex2(z.x), ex2(z.y)};
+            sum = add2(sum, w);
+            p[e / 2] = pack2(w.x, w.y);
+          }
+          st16(ts + j / 2, p);
         }
-        st16(tmem + lanes + j / 2, p);
+        l += sum.x + sum.y;
+        st_wait();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.p_full[x]);
       }
-      l += sum[0] + sum[1];
-      st_wait();
-      fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.p_full);
-    }
-    if (ok && i0 < i1) ok = all_sync(mbar_wait(&ctl.o_full, 0, abort_flag));
-    if (ok) {
+      if (ok && u.i0 < u.i1) ok = all_sync(mbar_wait(&ctl.o_full[x], nu++ & 1, abort_flag));
+      if (!ok) break;
       fence_after_sync();
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const size_t at = t.splits == 1 ? 0 : ((size_t)split * a.n_heads + h) * a.rows + qrow + r;
-      bf16* dst = (bf16*)a.out + (size_t)(qrow + r) * a.ldo + (size_t)h * D;
+      const size_t row = (size_t)u.qrow(x) + r, at = ((size_t)u.split * a.n_heads + u.h) * a.rows + row;
+      bf16* dst = (bf16*)a.out + row * a.ldo + (size_t)u.h * D;
       float odd = l * 0.f;                   // no number once a sum is not finite
-#pragma unroll 1
+#pragma unroll
       for (int j = 0; j < D; j += 32) {
         uint32_t o[32];
         float y[32];
-        if (i0 < i1) {
-          ld32(t_o + lanes + j, o);
+        if (u.i0 < u.i1) {
+          ld32(to + j, o);
           ld_wait();
         } else {
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0;
+        }
+        if (j + 32 == D && u.i0 < u.i1) {    // read back: the next unit's products may overwrite it
+          fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctl.o_empty[x]);
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
@@ -462,16 +590,16 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
       }
       if (r < rows) {
         const float lse = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
-        if (t.splits == 1) a.lse[(size_t)h * a.rows + qrow + r] = lse;
+        if (t.splits == 1) a.lse[(size_t)u.h * a.rows + row] = lse;
         else t.part_l[at] = lse;
       }
       unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f);
       __syncwarp();
-      for (; bad; bad &= bad - 1) fwd_row<D>(s, a, t, w, h, 32 * q + __ffs(bad) - 1, qrow, i0, i1, split);
+      for (; bad; bad &= bad - 1) fwd_row<D>(a, t, u, x, 32 * q + __ffs(bad) - 1);
     }
     fence_before_sync();
   }
-  finish(tid, warp, abort_flag, a.status, tmem, F::cols);
+  finish(tid, warp, abort_flag, a.status, tmem, 512);
 }
 
 // Joins the parts of a row's keys: a warp per (row, head).
@@ -504,36 +632,40 @@ __global__ void __launch_bounds__(256) k_gat_join(const __grid_constant__ AttnAr
 }
 
 // ---- backward: dq -------------------------------------------------------------------------------------
-// One block an SM.  S lies in two buffers and is issued two tiles ahead; dS takes dP's columns, each half of the
-// keys (64 columns, one group of four warps) in its own.  While the warps turn dP of a tile into dS, nothing of it is
-// behind them in the tensor cores' queue but the next tile's S.
+// A persistent block an SM, one query tile of a head at a time.  Two groups of four warps share a tile's rows, half of the
+// keys each.  The scores pass through registers, so that the next tile's are formed as soon as they are read; dP has
+// two buffers, and dS takes dP's columns (each half its own): the tensor cores work on S, dP of the next tile and dQ of the
+// last one while the warps turn this one's into dS.
 template <int D>
 struct Dq {
   static constexpr int NK = 3, NV = 2, threads = 320;
   static constexpr int smem = (2 + NK + NV) * kTileBytes<D> + 2048;
 };
 struct DqCtl {
-  uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2], q_full, s_full[2], dp_full, ds_full, o_full;
+  uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2], q_full, q_empty, s_full, s_empty, dp_full[2], ds_full, o_full, o_empty;
   uint32_t tmem;
   int abort_flag;
 };
 
+// Columns [half D/2, ..) of row r of the query tile, by one warp and over the keys the row sees alone.
 template <int D>
-__device__ __noinline__ void dq_row(const AttnArgs& a, const KeyWalk& w, int h, int r, int qrow, int i0, int i1, float* part) {
-  const int lane = threadIdx.x & 31;
+__device__ __noinline__ void dq_row(const AttnArgs& a, const TcArgs& t, const QueryWork<1> u, int r, int half) {
+  const int lane = threadIdx.x & 31, h = u.h;
+  const size_t row_q = (size_t)u.qrow(0) + r;
+  const TileRow tr(r, u.w.R);
   const bf16 *k = (const bf16*)a.k + (size_t)(h / a.per) * D, *v = (const bf16*)a.v + (size_t)(h / a.per) * D;
   float q[D / 32], g[D / 32], o[D / 32];
-  lane_load<D>((const bf16*)a.q + (size_t)(qrow + r) * a.ldq + (size_t)h * D, lane, q);
-  lane_load<D>((const bf16*)a.dout + (size_t)(qrow + r) * a.lddo + (size_t)h * D, lane, g);
-  const float lse = a.lse[(size_t)h * a.rows + qrow + r], delta = a.delta[(size_t)h * a.rows + qrow + r];
+  lane_load<D>((const bf16*)a.q + row_q * a.ldq + (size_t)h * D, lane, q);
+  lane_load<D>((const bf16*)a.dout + row_q * a.lddo + (size_t)h * D, lane, g);
+  const float lse = a.lse[(size_t)h * a.rows + row_q], delta = a.delta[(size_t)h * a.rows + row_q];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-  for (int i = i0; i < i1; ++i) {
+  for (int i = u.i0; i < u.i1; ++i) {
     int x0, n, lo, hi;
-    const int kind = w.tile(i, x0, n);
-    w.sees(kind, x0, n, r, lo, hi);
+    const int kind = u.w.tile(i, u.group(0), u.rows(0), x0, n);
+    tr.sees(kind, x0, n, u.group(0), u.rows(0), lo, hi);
     for (int c = lo; c <= hi; ++c) {
-      const size_t row = w.key_row(kind, x0 + c);
+      const size_t row = u.w.key_row(kind, x0 + c);
       float x[D / 32], y[D / 32];
       lane_load<D>(k + row * a.ldk, lane, x);
       lane_load<D>(v + row * a.ldv, lane, y);
@@ -542,13 +674,13 @@ __device__ __noinline__ void dq_row(const AttnArgs& a, const KeyWalk& w, int h, 
       for (int e = 0; e < D / 32; ++e) o[e] = fmaf(ds, x[e], o[e]);
     }
   }
-  if (part) {
+  float* part = t.part_o + (((size_t)u.split * a.n_heads + h) * a.rows + row_q) * D;
+  bf16* dst = (bf16*)a.dq + row_q * a.lddq + (size_t)h * D;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) part[lane + 32 * e] = o[e] * a.scale;
-  } else {
-    bf16* dst = (bf16*)a.dq + (size_t)(qrow + r) * a.lddq + (size_t)h * D;
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * a.scale);
+  for (int e = 0; e < D / 32; ++e) {
+    if (e / (D / 64) != half) continue;
+    if (t.splits > 1) part[lane + 32 * e] = o[e] * a.scale;
+    else dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * a.scale);
   }
 }
 
@@ -561,22 +693,23 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t sq = base, so = sq + kTileBytes<D>, sk = so + kTileBytes<D>, sv = sk + F::NK * kTileBytes<D>;
   DqCtl& ctl = *reinterpret_cast<DqCtl*>(smem_raw + (base - raw) + (2 + F::NK + F::NV) * kTileBytes<D>);
-  __shared__ unsigned s_bad[4];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < F::NK; ++i) { mbar_init(&ctl.k_full[i], 1); mbar_init(&ctl.k_empty[i], 1); }
     for (int i = 0; i < F::NV; ++i) { mbar_init(&ctl.v_full[i], 1); mbar_init(&ctl.v_empty[i], 1); }
     mbar_init(&ctl.q_full, 2);
-    mbar_init(&ctl.s_full[0], 1);
-    mbar_init(&ctl.s_full[1], 1);
-    mbar_init(&ctl.dp_full, 1);
+    mbar_init(&ctl.q_empty, 1);
+    mbar_init(&ctl.s_full, 1);
+    mbar_init(&ctl.s_empty, 8);
+    mbar_init(&ctl.dp_full[0], 1);
+    mbar_init(&ctl.dp_full[1], 1);
     mbar_init(&ctl.ds_full, 8);
     mbar_init(&ctl.o_full, 1);
+    mbar_init(&ctl.o_empty, 8);
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
   }
-  if (tid < 4) s_bad[tid] = 0;
   if (warp == 1) {
     __syncwarp();
     alloc_tmem(&ctl.tmem, 512);
@@ -584,113 +717,148 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
   }
   __syncthreads();
   fence_after_sync();
-  const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_dp = tmem + 2 * kT, t_o = tmem + 3 * kT;
+  const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_dp = tmem + kT, t_o = tmem + 3 * kT;
   volatile int* abort_flag = &ctl.abort_flag;
-  const int u = (int)(gridDim.x - 1 - blockIdx.x), tile = u / a.n_heads, h = u - tile * a.n_heads, split = blockIdx.y, b = seq_of_tile(s, tile);
-  const int gpt = groups_per_tile(kT, s.R), g0 = (tile - s.tile0[b]) * gpt, rows = min(gpt, s.groups[b] - g0) * s.R;
-  const KeyWalk w(s, b, g0 * s.R, rows);
-  const int qrow = s.q0[b] + w.rho0, i0 = w.total * split / t.splits, i1 = w.total * (split + 1) / t.splits, cnt = i1 - i0;
+  const int units = QueryWork<1>::count(s, a, t);
   pdl_wait();
 
   if (warp == 0) {
-    if (lane == 0 && cnt > 0) {
-      load_rows<D>(sq, &maps.q, qrow, h * D, &ctl.q_full);
-      load_rows<D>(so, &maps.dout, qrow, h * D, &ctl.q_full);
-      const int col = h / a.per * D;
-      for (int i = 0; i < cnt; ++i) {
-        int x0, n;
-        const int kind = w.tile(i0 + i, x0, n), row0 = kind == CTX ? w.kv0 : w.g0, ks = i % F::NK, vs = i % F::NV;
-        if (!mbar_wait(&ctl.k_empty[ks], ((i / F::NK) & 1) ^ 1, abort_flag)) break;
-        load_keys<D>(sk + ks * kTileBytes<D>, &maps.k, &maps.ks, kind, row0, s.R, x0, col, &ctl.k_full[ks]);
-        if (!mbar_wait(&ctl.v_empty[vs], ((i / F::NV) & 1) ^ 1, abort_flag)) break;
-        load_keys<D>(sv + vs * kTileBytes<D>, &maps.v, &maps.vs, kind, row0, s.R, x0, col, &ctl.v_full[vs]);
+    if (lane == 0) {
+      int it = 0, nu = 0;
+      bool ok = true;
+      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+        const QueryWork<1> u(s, a, t, unit);
+        if (u.i0 == u.i1) continue;
+        ok = mbar_wait(&ctl.q_empty, (nu++ & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        load_rows<D>(sq, &maps.q, u.qrow(0), u.h * D, &ctl.q_full);
+        load_rows<D>(so, &maps.dout, u.qrow(0), u.h * D, &ctl.q_full);
+        const int col = u.h / a.per * D;
+        for (int i = u.i0; i < u.i1; ++i, ++it) {
+          int x0, n;
+          const int kind = u.w.tile(i, u.group(0), u.rows(0), x0, n), row0 = kind == CTX ? u.w.kv0 : u.w.g0, ks = it % F::NK, vs = it % F::NV;
+          ok = mbar_wait(&ctl.k_empty[ks], ((it / F::NK) & 1) ^ 1, abort_flag);
+          if (!ok) break;
+          load_keys<D>(sk + ks * kTileBytes<D>, &maps.k, &maps.ks, kind, row0, s.R, x0, col, &ctl.k_full[ks]);
+          ok = mbar_wait(&ctl.v_empty[vs], ((it / F::NV) & 1) ^ 1, abort_flag);
+          if (!ok) break;
+          load_keys<D>(sv + vs * kTileBytes<D>, &maps.v, &maps.vs, kind, row0, s.R, x0, col, &ctl.v_full[vs]);
+        }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && cnt > 0) {
-      auto scores = [&](int i) {
-        const int ks = i % F::NK;
-        if (!mbar_wait(&ctl.k_full[ks], (i / F::NK) & 1, abort_flag)) return false;
+    if (lane == 0) {
+      int it = 0, nu = 0;   // tiles and units so far
+      bool ok = true;
+      // S and dP of tile number i (over all units)
+      auto issue = [&](int i, bool last) {
+        const int ks = i % F::NK, vs = i % F::NV;
+        ok = mbar_wait(&ctl.s_empty, (i & 1) ^ 1, abort_flag) && mbar_wait(&ctl.k_full[ks], (i / F::NK) & 1, abort_flag);
+        if (!ok) return;
         fence_after_sync();
-        mma_scores<D>(tmem + (i & 1) * kT, sq, sk + ks * kTileBytes<D>);
-        mma_commit(&ctl.s_full[i & 1]);
-        return true;
-      };
-      auto dprob = [&](int i) {
-        const int vs = i % F::NV;
-        if (!mbar_wait(&ctl.v_full[vs], (i / F::NV) & 1, abort_flag)) return false;
+        mma_scores<D>(tmem, desc_k(sq), desc_k(sk + ks * kTileBytes<D>));
+        mma_commit(&ctl.s_full);
+        ok = mbar_wait(&ctl.v_full[vs], (i / F::NV) & 1, abort_flag);
+        if (!ok) return;
         fence_after_sync();
-        mma_scores<D>(t_dp, so, sv + vs * kTileBytes<D>);
-        mma_commit(&ctl.dp_full);
+        mma_scores<D>(t_dp + (i & 1) * kT, desc_k(so), desc_k(sv + vs * kTileBytes<D>));
+        mma_commit(&ctl.dp_full[i & 1]);
         mma_commit(&ctl.v_empty[vs]);
-        return true;
+        if (last) mma_commit(&ctl.q_empty);
       };
-      bool ok = mbar_wait(&ctl.q_full, 0, abort_flag) && scores(0) && dprob(0) && (cnt < 2 || scores(1));
-      for (int i = 0; ok && i < cnt; ++i) {
-        if (!mbar_wait(&ctl.ds_full, i & 1, abort_flag)) break;
-        fence_after_sync();
-        const int ks = i % F::NK;
-        mma_sums<D>(t_o, t_dp, 64, sk + ks * kTileBytes<D>, i > 0);
-        mma_commit(&ctl.k_empty[ks]);
-        if (i + 1 < cnt) ok = dprob(i + 1);
-        else mma_commit(&ctl.o_full);
-        if (ok && i + 2 < cnt) ok = scores(i + 2);
+      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+        const QueryWork<1> u(s, a, t, unit);
+        const int cnt = u.i1 - u.i0;
+        if (cnt == 0) continue;
+        ok = mbar_wait(&ctl.q_full, nu & 1, abort_flag);
+        if (ok) issue(it, cnt == 1);
+        for (int i = 0; ok && i < cnt; ++i, ++it) {
+          if (i + 1 < cnt) issue(it + 1, i + 2 == cnt);
+          ok = ok && mbar_wait(&ctl.ds_full, it & 1, abort_flag);
+          if (ok && i == 0) ok = mbar_wait(&ctl.o_empty, (nu & 1) ^ 1, abort_flag);
+          if (!ok) break;
+          fence_after_sync();
+          const int ks = it % F::NK;
+          mma_sums<D>(t_o, t_dp + (it & 1) * kT, 64, desc_mn(sk + ks * kTileBytes<D>), i > 0);
+          mma_commit(&ctl.k_empty[ks]);
+          if (i + 1 == cnt) mma_commit(&ctl.o_full);
+        }
+        ++nu;
       }
     }
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2, r = 32 * q + lane;
-    const uint32_t lanes = (uint32_t)(32 * q) << 16;
+    const uint32_t lanes = (uint32_t)(32 * q) << 16, mine = lanes + 64 * half;
     const float c = a.scale * kLog2e;
-    const size_t at = (size_t)h * a.rows + qrow + r;
-    const float lse = r < rows ? a.lse[at] * kLog2e : 0.f, delta = r < rows ? a.delta[at] : 0.f;
+    const TileRow tr(r, s.R);
+    int it = 0, nu = 0;
     bool ok = true;
-    for (int i = 0; i < cnt; ++i) {
-      int x0, n, lo, hi;
-      const int kind = w.tile(i0 + i, x0, n);
-      w.sees(kind, x0, n, r, lo, hi);
-      lo -= 64 * half;
-      hi -= 64 * half;
-      ok = all_sync(mbar_wait(&ctl.s_full[i & 1], (i >> 1) & 1, abort_flag));
-      if (!ok) break;
-      fence_after_sync();
-      uint32_t v[64];
-      ld32(tmem + (i & 1) * kT + lanes + 64 * half, v);
-      ld32(tmem + (i & 1) * kT + lanes + 64 * half + 32, v + 32);
-      ld_wait();
-#pragma unroll
-      for (int j = 0; j < 64; ++j) v[j] = __float_as_uint(ex2(fmaf(__uint_as_float(v[j]), c, -lse)));
-      const bool whole = all_sync(lo <= 0 && hi >= 63);
-      ok = all_sync(mbar_wait(&ctl.dp_full, i & 1, abort_flag));
-      if (!ok) break;
-      fence_after_sync();
-#pragma unroll
-      for (int j = 0; j < 64; j += 32) {
-        uint32_t d[32], p[16];
-        ld32(t_dp + lanes + 64 * half + j, d);
+    for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      const QueryWork<1> u(s, a, t, unit);
+      const int rows = u.rows(0), cnt = u.i1 - u.i0;
+      const size_t row = (size_t)u.qrow(0) + r, at = (size_t)u.h * a.rows + row;
+      const float lse = r < rows ? a.lse[at] * kLog2e : 0.f, delta = r < rows ? a.delta[at] : 0.f;
+      for (int i = u.i0; i < u.i1; ++i, ++it) {
+        int x0, n, lo, hi;
+        const int kind = u.w.tile(i, u.group(0), rows, x0, n);
+        tr.sees(kind, x0, n, u.group(0), rows, lo, hi);
+        lo -= 64 * half;
+        hi -= 64 * half;
+        ok = all_sync(mbar_wait(&ctl.s_full, it & 1, abort_flag));
+        if (!ok) break;
+        fence_after_sync();
+        uint32_t v[64];
+        ld32(tmem + mine, v);
+        ld32(tmem + mine + 32, v + 32);
         ld_wait();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.s_empty);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          float x = __uint_as_float(v[j + e]) * (__uint_as_float(d[e]) - delta);
-          if (!whole && (j + e < lo || j + e > hi)) x = 0.f;
-          d[e] = __float_as_uint(x);
+        for (int j = 0; j < 64; j += 2) {
+          const f2 z = fma2(pair_of(v + j), f2{c, c}, f2{-lse, -lse});
+          v[j] = __float_as_uint(ex2(z.x));
+          v[j + 1] = __float_as_uint(ex2(z.y));
         }
+        const bool whole = all_sync(lo <= 0 && hi >= 63);
+        const uint32_t td = t_dp + (it & 1) * kT + mine;
+        ok = all_sync(mbar_wait(&ctl.dp_full[it & 1], (it >> 1) & 1, abort_flag));
+        if (!ok) break;
+        fence_after_sync();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) p[e] = pack2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
-        st16(t_dp + lanes + 64 * half + j / 2, p);
+        for (int j = 0; j < 64; j += 32) {
+          uint32_t d[32], p[16];
+          ld32(td + j, d);
+          ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const f2 z = mul2(pair_of(v + j + e), add2(pair_of(d + e), f2{-delta, -delta}));
+            d[e] = __float_as_uint(z.x);
+            d[e + 1] = __float_as_uint(z.y);
+          }
+          if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (j + e < lo || j + e > hi) d[e] = 0;
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[e] = pack2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+          st16(td + j / 2, p);
+        }
+        st_wait();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.ds_full);
       }
-      st_wait();
-      fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.ds_full);
-    }
-    if (ok && cnt > 0) ok = all_sync(mbar_wait(&ctl.o_full, 0, abort_flag));
-    float* part = t.splits == 1 ? nullptr : t.part_o + (((size_t)split * a.n_heads + h) * a.rows + qrow) * D;
-    if (ok) {
+      if (ok && cnt > 0) ok = all_sync(mbar_wait(&ctl.o_full, nu++ & 1, abort_flag));
+      if (!ok) break;
       fence_after_sync();
-      bf16* dst = (bf16*)a.dq + (size_t)(qrow + r) * a.lddq + (size_t)h * D;
+      float* part = t.part_o + (((size_t)u.split * a.n_heads + u.h) * a.rows + row) * D;
+      bf16* dst = (bf16*)a.dq + row * a.lddq + (size_t)u.h * D;
       float odd = 0.f;
 #pragma unroll
-      for (int j = half * (D / 2); j < (half + 1) * (D / 2); j += 32) {
+      for (int j0 = 0; j0 < D / 2; j0 += 32) {
+        const int j = half * (D / 2) + j0;
         uint32_t o[32];
         float y[32];
         if (cnt > 0) {
@@ -700,31 +868,29 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0;
         }
+        if (j0 + 32 == D / 2 && cnt > 0) {
+          fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctl.o_empty);
+        }
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
           odd = fmaf(__uint_as_float(o[e]), 0.f, odd);
           y[e] = __uint_as_float(o[e]) * a.scale;
         }
         if (r < rows) {
-          if (!part) {
+          if (t.splits == 1) {
             store_bf16<32>(dst + j, y);
           } else {
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(part + (size_t)r * D + j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+              *reinterpret_cast<float4*>(part + j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
           }
         }
       }
-      const unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f);
-      if (lane == 0 && bad) atomicOr(&s_bad[q], bad);
-    }
-    asm volatile("bar.sync 1, 256;" ::: "memory");   // the eight warps: a row's halves are both stored
-    if (ok) {
-      unsigned todo = half == 0 ? s_bad[q] : 0u;
-      for (; todo; todo &= todo - 1) {
-        const int rr = 32 * q + __ffs(todo) - 1;
-        dq_row<D>(a, w, h, rr, qrow, i0, i1, part ? part + (size_t)rr * D : nullptr);
-      }
+      unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f);
+      __syncwarp();
+      for (; bad; bad &= bad - 1) dq_row<D>(a, t, u, 32 * q + __ffs(bad) - 1, half);
     }
     fence_before_sync();
   }
@@ -751,59 +917,204 @@ __global__ void __launch_bounds__(256) k_gat_dq_join(const __grid_constant__ Att
   for (int e = 0; e < D / 32; ++e) dst[lane + 32 * e] = __float2bfloat16_rn(o[e]);
 }
 
+// ---- backward: dk, dv of the masks, delta ------------------------------------------------------------------
+// A [MASK] row is seen by the R - j rows of its own group that follow it: too little for a matrix product.  The lanes of
+// a (group, key head) keep the group's keys, values and their gradients in registers, C neighbouring channels
+// each; they also form delta = dout . out of the rows they read anyway.  Bound by memory.
+template <int C>
+struct Chans { uint32_t v[C / 2]; };   // C neighbouring channels, bf16
+template <int C>
+__device__ __forceinline__ Chans<C> chan_load(const bf16* p) {
+  Chans<C> r;
+  if constexpr (C == 8) {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    r.v[0] = x.x; r.v[1] = x.y; r.v[2] = x.z; r.v[3] = x.w;
+  } else if constexpr (C == 4) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    r.v[0] = x.x; r.v[1] = x.y;
+  } else {
+    r.v[0] = *reinterpret_cast<const uint32_t*>(p);
+  }
+  return r;
+}
+template <int C>
+__device__ __forceinline__ void chan_store(bf16* p, const float (&x)[C]) {
+  if constexpr (C == 8)
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+  else if constexpr (C == 4) *reinterpret_cast<uint2*>(p) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+  else *reinterpret_cast<uint32_t*>(p) = pack2(x[0], x[1]);
+}
+template <int C>
+__device__ __forceinline__ float chan(const Chans<C>& x, int e) {
+  return __uint_as_float(e % 2 ? x.v[e / 2] & 0xFFFF0000u : x.v[e / 2] << 16);
+}
+template <int C>
+__device__ __forceinline__ float chan_dot(const Chans<C>& x, const Chans<C>& y) {
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < C; ++e) s = fmaf(chan(x, e), chan(y, e), s);
+  return s;
+}
+
+// D / C lanes per (group, key head); RM: most rows of a group that the registers hold.
+template <int D, int RM, int C>
+__global__ void __launch_bounds__(128, RM <= 9 ? 3 : 2) k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, int groups) {
+  constexpr int L = D / C;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x % L, R = s.R;
+  const long long unit = ((long long)blockIdx.x * 128 + threadIdx.x) / L;
+  const bool there = unit < (long long)groups * a.n_kv;   // (all lanes of a warp take part in its exchanges)
+  const int g = there ? (int)(unit / a.n_kv) : 0, hk = there ? (int)(unit - (long long)g * a.n_kv) : 0;
+  int lo = 0, hi = s.B - 1;            // the sequence of group g: its rows begin at q0 / R
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (s.q0[mid] <= g * R) lo = mid; else hi = mid - 1;
+  }
+  const size_t q0 = (size_t)g * R, k0 = (size_t)s.kv0[lo] + s.ctx[lo] + (q0 - s.q0[lo]);
+  Chans<C> k[RM], v[RM];
+  float dk[RM][C], dv[RM][C];
+#pragma unroll
+  for (int j = 1; j < RM; ++j) {
+    if (j < R) {
+      k[j] = chan_load<C>((const bf16*)a.k + (k0 + j) * a.ldk + (size_t)hk * D + C * lane);
+      v[j] = chan_load<C>((const bf16*)a.v + (k0 + j) * a.ldv + (size_t)hk * D + C * lane);
+    }
+#pragma unroll
+    for (int e = 0; e < C; ++e) dk[j][e] = dv[j][e] = 0.f;
+  }
+  const float c = a.scale * kLog2e;
+  for (int h = hk * a.per; h < (hk + 1) * a.per; ++h) {
+    float* delta_out = a.delta + (size_t)h * a.rows + q0;
+    const float* lse_in = a.lse + (size_t)h * a.rows + q0;
+    const bf16 *q_in = (const bf16*)a.q + q0 * a.ldq + (size_t)h * D + C * lane,
+               *g_in = (const bf16*)a.dout + q0 * a.lddo + (size_t)h * D + C * lane,
+               *o_in = (const bf16*)a.out + q0 * a.ldo + (size_t)h * D + C * lane;
+    // four rows' values in flight
+    constexpr int NB = RM < 5 ? RM : (RM == 5 ? 5 : 4);
+#pragma unroll
+    for (int i0 = 0; i0 < RM; i0 += NB) {
+      if (i0 >= R) break;
+      Chans<C> q[NB], d[NB], o[NB];
+      float lse[NB];
+#pragma unroll
+      for (int x = 0; x < NB; ++x) {
+        const int i = i0 + x;
+        if (i < RM && i < R) {
+          d[x] = chan_load<C>(g_in + i * a.lddo);
+          o[x] = chan_load<C>(o_in + i * a.ldo);
+          if (i > 0) {
+            q[x] = chan_load<C>(q_in + i * a.ldq);
+            lse[x] = lse_in[i] * kLog2e;
+          }
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < NB; ++x) {
+        const int i = i0 + x;
+        if (i >= RM || i >= R) break;
+        float delta = chan_dot(d[x], o[x]);
+#pragma unroll
+        for (int w = L / 2; w > 0; w >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, w);
+        if (lane == 0 && there) delta_out[i] = delta;
+#pragma unroll
+        for (int j = 1; j < RM; ++j) {
+          if (j > i) break;
+          float sc = chan_dot(q[x], k[j]), dp = chan_dot(d[x], v[j]);
+#pragma unroll
+          for (int w = L / 2; w > 0; w >>= 1) {
+            sc += __shfl_xor_sync(0xffffffffu, sc, w);
+            dp += __shfl_xor_sync(0xffffffffu, dp, w);
+          }
+          const float p = ex2(fmaf(sc, c, -lse[x])), ds = p * (dp - delta);
+#pragma unroll
+          for (int e = 0; e < C; ++e) {
+            dv[j][e] = fmaf(p, chan(d[x], e), dv[j][e]);
+            dk[j][e] = fmaf(ds, chan(q[x], e), dk[j][e]);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 1; j < RM; ++j) {
+    if (j >= R || !there) break;
+#pragma unroll
+    for (int e = 0; e < C; ++e) dk[j][e] *= a.scale;
+    chan_store<C>((bf16*)a.dk + (k0 + j) * a.lddk + (size_t)hk * D + C * lane, dk[j]);
+    chan_store<C>((bf16*)a.dv + (k0 + j) * a.lddv + (size_t)hk * D + C * lane, dv[j]);
+  }
+}
+
 // ---- backward: dk, dv -----------------------------------------------------------------------------------
-// One block an SM with one key tile; steps over the query tiles of all heads that share the key head.  Tensor memory
-// is full with S^T (P^T in its columns), dP^T (dS^T in its columns), dK and dV.  The warps form P^T while the tensor
-// cores work on dK and dP^T, and dS^T while they work on dV and the next step's S^T.  A thread owns a key and half of
-// the query columns, whose lse and delta a warp of its own puts into shared memory.
+// A persistent block an SM, one key tile (context or real rows) and key head at a time, or a part of its steps:
+// the query tiles of all heads that share the key head.  Tensor memory is full with S^T (P^T in its columns), dP^T (dS^T
+// in its columns), dK and dV.  The warps form P^T while the tensor cores work on dK and dP^T, and dS^T while they work on
+// dV and the next step's S^T.  A thread owns a key and half of the query columns, whose lse and delta a warp
+// of its own puts into shared memory.
 template <int D>
 struct Dkv {
-  static constexpr int NQ = 2, threads = 352;
-  static constexpr int smem = (2 + 2 * NQ) * kTileBytes<D> + 1024 + 2 * 2 * kT * 4 + 1024;
+  static constexpr int threads = 352;
+  static constexpr int smem = 6 * kTileBytes<D> + 1024 + 2 * 2 * kT * 4 + 1024;
 };
 struct DkvCtl {
-  uint64_t q_full[2], q_empty[2], g_full[2], g_empty[2], t_full[2], t_empty[2], k_full, s_full, p_full, dp_full, ds_full, o_full;
+  uint64_t q_full[2], q_empty[2], g_full[2], g_empty[2], t_full[2], t_empty[2], k_full, k_empty, s_full, p_full, dp_full, ds_full,
+      o_full, o_empty;
   uint32_t tmem;
   int abort_flag;
 };
 
-// What a key tile is: its rows and the query rows [q_begin, q_end) of the sequence that see any of it.
-struct KeyTile {
-  int kind, x0, n, row0, step, q_begin, q_end;
-  __device__ KeyTile(const Seqs& s, int b, int i) {
-    const int ctx = s.ctx[b], groups = s.groups[b], R = s.R, gpt = groups_per_tile(kT, R);
-    const int n_ctx = div_up(ctx, kT), n_rt = div_up(groups, kT), g0 = s.kv0[b] + ctx;
+struct KeyWork {
+  int b, hk, part, parts, slot;        // slot: of its sums, if there is more than one part
+  int kind, x0, n, row0, step, q_begin, q_end, per_head, j0, j1;
+  __device__ static int count(const Seqs& s, const AttnArgs& a, const TcArgs& t) { return s.tile0[s.B] * a.n_kv * t.parts; }
+  __device__ KeyWork(const Seqs& s, const AttnArgs& a, const TcArgs& t, int unit) {
+    // (the first tiles of a sequence are seen by the most rows: parts of all heads side by side, tiles in order)
+    const int tile = unit / (a.n_kv * t.parts), i = unit - tile * a.n_kv * t.parts;
+    hk = i / t.parts;
+    part = i - hk * t.parts;
+    slot = unit;
+    b = seq_of_tile(s, tile);
+    const int ctx = s.ctx[b], groups = s.groups[b], R = s.R, x = tile - s.tile0[b], n_ctx = div_up(ctx, kT);
     step = 1;
     q_begin = 0;
     q_end = groups * R;
-    if (i < n_ctx) { kind = CTX; x0 = i * kT; n = min(kT, ctx - x0); row0 = s.kv0[b] + x0; }
-    else if (i < n_ctx + n_rt) { kind = REAL; x0 = (i - n_ctx) * kT; n = min(kT, groups - x0); step = R; row0 = g0 + x0 * R; q_begin = x0 * R; }
-    else { kind = LOCAL; x0 = (i - n_ctx - n_rt) * gpt * R; n = min(gpt * R, groups * R - x0); row0 = g0 + x0; q_begin = x0; q_end = x0 + n; }
+    if (x < n_ctx) { kind = CTX; x0 = x * kT; n = min(kT, ctx - x0); row0 = s.kv0[b] + x0; }
+    else { kind = REAL; x0 = (x - n_ctx) * kT; n = min(kT, groups - x0); step = R; row0 = s.kv0[b] + ctx + x0 * R; q_begin = x0 * R; }
+    per_head = div_up(q_end - q_begin, kT);
+    const int cnt = per_head * a.per;
+    parts = max(1, div_up(cnt, t.cap));
+    j0 = min(cnt, part * t.cap);
+    j1 = min(cnt, j0 + t.cap);
+    if (t.parts == 1) { parts = 1; j0 = 0; j1 = cnt; }
   }
-  // Query rows (of the sequence) that see key i of the tile: [lo, hi].
+  __device__ bool there() const { return part < parts; }
+  // Query row (of the sequence) and head of step j.
+  __device__ int head(int j, int per) const { return hk * per + j / per_head; }
+  __device__ int row(int j) const { return q_begin + j % per_head * kT; }
+  // Query rows that see key i of the tile: [lo, hi].
   __device__ void seen(int i, int R, int& lo, int& hi) const {
-    lo = q_begin;
-    hi = q_end - 1;
-    if (kind == REAL) lo = (x0 + i) * R;
-    if (kind == LOCAL) { lo = x0 + i; hi = x0 + i - i % R + R - 1; if (i % R == 0) hi = -1; }
-    if (i >= n) hi = -1;
+    lo = kind == REAL ? (x0 + i) * R : 0;
+    hi = i < n ? q_end - 1 : -1;
   }
 };
 
+// Columns [half D/2, ..) of dk and dv of key i of the tile, by one warp and over the rows that see it alone.
 template <int D>
-__device__ __noinline__ void dkv_row(const Seqs& s, const AttnArgs& a, const KeyTile& kt, int b, int hk, int i) {
+__device__ __noinline__ void dkv_row(const Seqs& s, const AttnArgs& a, const TcArgs& t, const KeyWork u, int i, int half) {
   const int lane = threadIdx.x & 31;
-  const size_t row = (size_t)kt.row0 + (size_t)i * kt.step;
+  const size_t row = (size_t)u.row0 + (size_t)i * u.step;
   float k[D / 32], v[D / 32], dk[D / 32], dv[D / 32];
-  lane_load<D>((const bf16*)a.k + row * a.ldk + (size_t)hk * D, lane, k);
-  lane_load<D>((const bf16*)a.v + row * a.ldv + (size_t)hk * D, lane, v);
+  lane_load<D>((const bf16*)a.k + row * a.ldk + (size_t)u.hk * D, lane, k);
+  lane_load<D>((const bf16*)a.v + row * a.ldv + (size_t)u.hk * D, lane, v);
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) dk[e] = dv[e] = 0.f;
   int lo, hi;
-  kt.seen(i, s.R, lo, hi);
-  for (int h = hk * a.per; h < (hk + 1) * a.per; ++h)
-    for (int r = lo; r <= hi; ++r) {
-      const size_t qr = (size_t)s.q0[b] + r;
+  u.seen(i, s.R, lo, hi);
+  for (int j = u.j0; j < u.j1; ++j) {
+    const int h = u.head(j, a.per), r0 = u.row(j);
+    for (int r = max(lo, r0); r <= min(hi, r0 + kT - 1); ++r) {
+      const size_t qr = (size_t)s.q0[u.b] + r;
       float x[D / 32], g[D / 32];
       lane_load<D>((const bf16*)a.q + qr * a.ldq + (size_t)h * D, lane, x);
       lane_load<D>((const bf16*)a.dout + qr * a.lddo + (size_t)h * D, lane, g);
@@ -815,24 +1126,31 @@ __device__ __noinline__ void dkv_row(const Seqs& s, const AttnArgs& a, const Key
         dk[e] = fmaf(ds, x[e], dk[e]);
       }
     }
-  bf16 *ok = (bf16*)a.dk + row * a.lddk + (size_t)hk * D, *ov = (bf16*)a.dv + row * a.lddv + (size_t)hk * D;
+  }
+  bf16 *ok = (bf16*)a.dk + row * a.lddk + (size_t)u.hk * D, *ov = (bf16*)a.dv + row * a.lddv + (size_t)u.hk * D;
+  float* part = t.part_o + ((size_t)u.slot * 2 * kT + i) * D;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) {
-    ok[lane + 32 * e] = __float2bfloat16_rn(dk[e] * a.scale);
-    ov[lane + 32 * e] = __float2bfloat16_rn(dv[e]);
+    if (e / (D / 64) != half) continue;
+    if (u.parts > 1) {
+      part[lane + 32 * e] = dk[e] * a.scale;
+      part[kT * D + lane + 32 * e] = dv[e];
+    } else {
+      ok[lane + 32 * e] = __float2bfloat16_rn(dk[e] * a.scale);
+      ov[lane + 32 * e] = __float2bfloat16_rn(dv[e]);
+    }
   }
 }
 
 template <int D>
 __global__ void __launch_bounds__(Dkv<D>::threads, 1)
-k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a) {
-  using F = Dkv<D>;
+k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a,
+          const __grid_constant__ TcArgs t) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t sk = base, sv = sk + kTileBytes<D>, sq = sv + kTileBytes<D>, sg = sq + F::NQ * kTileBytes<D>;
-  float* s_stat = reinterpret_cast<float*>(smem_raw + (base - raw) + (2 + 2 * F::NQ) * kTileBytes<D>);   // [slot][lse, delta][128]
+  const uint32_t sk = base, sv = sk + kTileBytes<D>, sq = sv + kTileBytes<D>, sg = sq + 2 * kTileBytes<D>;
+  float* s_stat = reinterpret_cast<float*>(smem_raw + (base - raw) + 6 * kTileBytes<D>);   // [slot][-lse, -delta][128]
   DkvCtl& ctl = *reinterpret_cast<DkvCtl*>(s_stat + 2 * 2 * kT);
-  __shared__ unsigned s_bad[4];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -841,16 +1159,17 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
       mbar_init(&ctl.t_full[i], 32); mbar_init(&ctl.t_empty[i], 8);
     }
     mbar_init(&ctl.k_full, 2);
+    mbar_init(&ctl.k_empty, 1);
     mbar_init(&ctl.s_full, 1);
     mbar_init(&ctl.p_full, 8);
     mbar_init(&ctl.dp_full, 1);
     mbar_init(&ctl.ds_full, 8);
     mbar_init(&ctl.o_full, 1);
+    mbar_init(&ctl.o_empty, 8);
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
   }
-  if (tid < 4) s_bad[tid] = 0;
   if (warp == 1) {
     __syncwarp();
     alloc_tmem(&ctl.tmem, 512);
@@ -860,255 +1179,376 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
   fence_after_sync();
   const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_dp = tmem + kT, t_dk = tmem + 2 * kT, t_dv = tmem + 3 * kT;
   volatile int* abort_flag = &ctl.abort_flag;
-  const int tile = blockIdx.x / a.n_kv, hk = blockIdx.x - tile * a.n_kv, b = seq_of_tile(s, tile);
-  const KeyTile kt(s, b, tile - s.tile0[b]);
-  const int per_head = div_up(kt.q_end - kt.q_begin, kT), cnt = per_head * a.per;
+  const int units = KeyWork::count(s, a, t);
   pdl_wait();
 
   if (warp == 0) {
-    if (lane == 0 && cnt > 0) {
-      const int row0 = kt.kind == CTX ? s.kv0[b] : s.kv0[b] + s.ctx[b];
-      load_keys<D>(sk, &maps.k, &maps.ks, kt.kind, row0, s.R, kt.x0, hk * D, &ctl.k_full);
-      load_keys<D>(sv, &maps.v, &maps.vs, kt.kind, row0, s.R, kt.x0, hk * D, &ctl.k_full);
-      for (int i = 0; i < cnt; ++i) {
-        const int hh = i / per_head, r0 = s.q0[b] + kt.q_begin + (i - hh * per_head) * kT, col = (hk * a.per + hh) * D, slot = i & 1;
-        const uint32_t parity = ((i >> 1) & 1) ^ 1;
-        if (!mbar_wait(&ctl.q_empty[slot], parity, abort_flag)) break;
-        load_rows<D>(sq + slot * kTileBytes<D>, &maps.q, r0, col, &ctl.q_full[slot]);
-        if (!mbar_wait(&ctl.g_empty[slot], parity, abort_flag)) break;
-        load_rows<D>(sg + slot * kTileBytes<D>, &maps.dout, r0, col, &ctl.g_full[slot]);
+    if (lane == 0) {
+      int it = 0, nu = 0;
+      bool ok = true;
+      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+        const KeyWork u(s, a, t, unit);
+        if (!u.there() || u.j0 == u.j1) continue;
+        ok = mbar_wait(&ctl.k_empty, (nu++ & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        const int base_row = u.kind == CTX ? s.kv0[u.b] : s.kv0[u.b] + s.ctx[u.b];
+        load_keys<D>(sk, &maps.k, &maps.ks, u.kind, base_row, s.R, u.x0, u.hk * D, &ctl.k_full);
+        load_keys<D>(sv, &maps.v, &maps.vs, u.kind, base_row, s.R, u.x0, u.hk * D, &ctl.k_full);
+        for (int j = u.j0; j < u.j1; ++j, ++it) {
+          const int r0 = s.q0[u.b] + u.row(j), col = u.head(j, a.per) * D, slot = it & 1;
+          const uint32_t parity = ((it >> 1) & 1) ^ 1;
+          ok = mbar_wait(&ctl.q_empty[slot], parity, abort_flag);
+          if (!ok) break;
+          load_rows<D>(sq + slot * kTileBytes<D>, &maps.q, r0, col, &ctl.q_full[slot]);
+          ok = mbar_wait(&ctl.g_empty[slot], parity, abort_flag);
+          if (!ok) break;
+          load_rows<D>(sg + slot * kTileBytes<D>, &maps.dout, r0, col, &ctl.g_full[slot]);
+        }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && cnt > 0) {
+    if (lane == 0) {
+      int it = 0, nu = 0;
+      bool ok = true;
       auto scores = [&](int i) {
-        if (!mbar_wait(&ctl.q_full[i & 1], (i >> 1) & 1, abort_flag)) return false;
+        ok = ok && mbar_wait(&ctl.q_full[i & 1], (i >> 1) & 1, abort_flag);
+        if (!ok) return;
         fence_after_sync();
-        mma_scores<D>(tmem, sk, sq + (i & 1) * kTileBytes<D>);
+        mma_scores<D>(tmem, desc_k(sk), desc_k(sq + (i & 1) * kTileBytes<D>));
         mma_commit(&ctl.s_full);
-        return true;
       };
-      auto dprob = [&](int i) {
-        if (!mbar_wait(&ctl.g_full[i & 1], (i >> 1) & 1, abort_flag)) return false;
+      auto dprob = [&](int i, bool last) {
+        ok = ok && mbar_wait(&ctl.g_full[i & 1], (i >> 1) & 1, abort_flag);
+        if (!ok) return;
         fence_after_sync();
-        mma_scores<D>(t_dp, sv, sg + (i & 1) * kTileBytes<D>);
+        mma_scores<D>(t_dp, desc_k(sv), desc_k(sg + (i & 1) * kTileBytes<D>));
         mma_commit(&ctl.dp_full);
-        return true;
+        if (last) mma_commit(&ctl.k_empty);
       };
-      bool ok = mbar_wait(&ctl.k_full, 0, abort_flag) && scores(0) && dprob(0);
-      for (int i = 0; ok && i < cnt; ++i) {
-        if (!mbar_wait(&ctl.p_full, i & 1, abort_flag)) break;
-        fence_after_sync();
-        mma_sums<D>(t_dv, tmem, 64, sg + (i & 1) * kTileBytes<D>, i > 0);
-        mma_commit(&ctl.g_empty[i & 1]);
-        if (i + 1 < cnt && !scores(i + 1)) break;
-        if (!mbar_wait(&ctl.ds_full, i & 1, abort_flag)) break;
-        fence_after_sync();
-        mma_sums<D>(t_dk, t_dp, 64, sq + (i & 1) * kTileBytes<D>, i > 0);
-        mma_commit(&ctl.q_empty[i & 1]);
-        if (i + 1 < cnt) ok = dprob(i + 1);
-        else mma_commit(&ctl.o_full);
+      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+        const KeyWork u(s, a, t, unit);
+        const int cnt = u.j1 - u.j0;
+        if (!u.there() || cnt == 0) continue;
+        ok = mbar_wait(&ctl.k_full, nu & 1, abort_flag);
+        scores(it);
+        dprob(it, cnt == 1);
+        for (int i = 0; ok && i < cnt; ++i, ++it) {
+          ok = mbar_wait(&ctl.p_full, it & 1, abort_flag);
+          if (ok && i == 0) ok = mbar_wait(&ctl.o_empty, (nu & 1) ^ 1, abort_flag);
+          if (!ok) break;
+          fence_after_sync();
+          mma_sums<D>(t_dv, tmem, 64, desc_mn(sg + (it & 1) * kTileBytes<D>), i > 0);
+          mma_commit(&ctl.g_empty[it & 1]);
+          if (i + 1 < cnt) scores(it + 1);
+          ok = ok && mbar_wait(&ctl.ds_full, it & 1, abort_flag);
+          if (!ok) break;
+          fence_after_sync();
+          mma_sums<D>(t_dk, t_dp, 64, desc_mn(sq + (it & 1) * kTileBytes<D>), i > 0);
+          mma_commit(&ctl.q_empty[it & 1]);
+          if (i + 1 < cnt) dprob(it + 1, i + 2 == cnt);
+          else mma_commit(&ctl.o_full);
+        }
+        ++nu;
       }
     }
   } else if (warp == 2) {
-    for (int i = 0; i < cnt; ++i) {
-      const int hh = i / per_head, r0 = kt.q_begin + (i - hh * per_head) * kT, slot = i & 1;
-      if (!all_sync(mbar_wait(&ctl.t_empty[slot], ((i >> 1) & 1) ^ 1, abort_flag))) break;
-      const size_t at = (size_t)(hk * a.per + hh) * a.rows + s.q0[b] + r0;
+    int it = 0;
+    bool ok = true;
+    for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      const KeyWork u(s, a, t, unit);
+      if (!u.there()) continue;
+      for (int j = u.j0; j < u.j1; ++j, ++it) {
+        const int r0 = u.row(j), slot = it & 1;
+        ok = all_sync(mbar_wait(&ctl.t_empty[slot], ((it >> 1) & 1) ^ 1, abort_flag));
+        if (!ok) break;
+        const size_t at = (size_t)u.head(j, a.per) * a.rows + s.q0[u.b] + r0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int col = lane + 32 * e;
-        const bool in = r0 + col < kt.q_end;
-        s_stat[(2 * slot) * kT + col] = in ? a.lse[at + col] * kLog2e : 0.f;
-        s_stat[(2 * slot + 1) * kT + col] = in ? a.delta[at + col] : 0.f;
+        for (int e = 0; e < 4; ++e) {
+          const int col = lane + 32 * e;
+          const bool in = r0 + col < u.q_end;
+          s_stat[(2 * slot) * kT + col] = in ? a.lse[at + col] * -kLog2e : 0.f;
+          s_stat[(2 * slot + 1) * kT + col] = in ? -a.delta[at + col] : 0.f;
+        }
+        mbar_arrive(&ctl.t_full[slot]);
       }
-      mbar_arrive(&ctl.t_full[slot]);
     }
   } else {
     const int q = warp & 3, half = (warp - 3) >> 2, key = 32 * q + lane;
-    const uint32_t lanes = (uint32_t)(32 * q) << 16;
+    const uint32_t lanes = (uint32_t)(32 * q) << 16, mine = lanes + 64 * half;
     const float c = a.scale * kLog2e;
-    int see0, see1;
-    kt.seen(key, s.R, see0, see1);
+    int it = 0, nu = 0;
     bool ok = true;
-    for (int i = 0; i < cnt; ++i) {
-      const int hh = i / per_head, r0 = kt.q_begin + (i - hh * per_head) * kT + 64 * half, slot = i & 1;
-      const int lo = see0 - r0, hi = see1 - r0;
-      const bool whole = all_sync(lo <= 0 && hi >= 63);
-      const float4 *lse = reinterpret_cast<const float4*>(s_stat + (2 * slot) * kT + 64 * half),
-                   *delta = reinterpret_cast<const float4*>(s_stat + (2 * slot + 1) * kT + 64 * half);
-      ok = all_sync(mbar_wait(&ctl.t_full[slot], (i >> 1) & 1, abort_flag)) && all_sync(mbar_wait(&ctl.s_full, i & 1, abort_flag));
-      if (!ok) break;
-      fence_after_sync();
-      uint32_t v[64];
-      ld32(tmem + lanes + 64 * half, v);
-      ld32(tmem + lanes + 64 * half + 32, v + 32);
-      ld_wait();
-#pragma unroll
-      for (int j = 0; j < 64; j += 4) {
-        const float4 y = lse[j / 4];
-        const float yy[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float p = ex2(fmaf(__uint_as_float(v[j + e]), c, -yy[e]));
-          if (!whole && (j + e < lo || j + e > hi)) p = 0.f;
-          v[j + e] = __float_as_uint(p);
-        }
-      }
-      {
-        uint32_t p[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) p[e] = pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
-        st32(tmem + lanes + 64 * half, p);
-      }
-      st_wait();
-      fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.p_full);
-      ok = all_sync(mbar_wait(&ctl.dp_full, i & 1, abort_flag));
-      if (!ok) break;
-      fence_after_sync();
-#pragma unroll
-      for (int j = 0; j < 64; j += 32) {
-        uint32_t d[32], p[16];
-        ld32(t_dp + lanes + 64 * half + j, d);
+    for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      const KeyWork u(s, a, t, unit);
+      if (!u.there()) continue;
+      const int cnt = u.j1 - u.j0;
+      int see0, see1;
+      u.seen(key, s.R, see0, see1);
+      for (int j = u.j0; j < u.j1; ++j, ++it) {
+        const int r0 = u.row(j) + 64 * half, slot = it & 1, lo = see0 - r0, hi = see1 - r0;
+        const bool whole = all_sync(lo <= 0 && hi >= 63);
+        const float4 *lse = reinterpret_cast<const float4*>(s_stat + (2 * slot) * kT + 64 * half),
+                     *delta = reinterpret_cast<const float4*>(s_stat + (2 * slot + 1) * kT + 64 * half);
+        ok = all_sync(mbar_wait(&ctl.t_full[slot], (it >> 1) & 1, abort_flag)) && all_sync(mbar_wait(&ctl.s_full, it & 1, abort_flag));
+        if (!ok) break;
+        fence_after_sync();
+        uint32_t v[64];
+        ld32(tmem + mine, v);
+        ld32(tmem + mine + 32, v + 32);
         ld_wait();
 #pragma unroll
-        for (int e = 0; e < 32; e += 4) {
-          const float4 y = delta[(j + e) / 4];
-          const float yy[4] = {y.x, y.y, y.z, y.w};
-          float x[4];
-#pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            x[f] = __uint_as_float(v[j + e + f]) * (__uint_as_float(d[e + f]) - yy[f]);
-            if (!whole && (j + e + f < lo || j + e + f > hi)) x[f] = 0.f;
-          }
-          p[e / 2] = pack2(x[0], x[1]);
-          p[e / 2 + 1] = pack2(x[2], x[3]);
+        for (int i = 0; i < 64; i += 4) {
+          const float4 y = lse[i / 4];
+          const f2 z0 = fma2(pair_of(v + i), f2{c, c}, f2{y.x, y.y}), z1 = fma2(pair_of(v + i + 2), f2{c, c}, f2{y.z, y.w});
+          v[i] = __float_as_uint(ex2(z0.x));
+          v[i + 1] = __float_as_uint(ex2(z0.y));
+          v[i + 2] = __float_as_uint(ex2(z1.x));
+          v[i + 3] = __float_as_uint(ex2(z1.y));
         }
-        st16(t_dp + lanes + 64 * half + j / 2, p);
+        if (!whole) {
+#pragma unroll
+          for (int i = 0; i < 64; ++i)
+            if (i < lo || i > hi) v[i] = 0;
+        }
+        {
+          uint32_t p[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) p[e] = pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+          st32(tmem + mine, p);
+        }
+        st_wait();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.p_full);
+        ok = all_sync(mbar_wait(&ctl.dp_full, it & 1, abort_flag));
+        if (!ok) break;
+        fence_after_sync();
+#pragma unroll
+        for (int i = 0; i < 64; i += 32) {
+          uint32_t d[32], p[16];
+          ld32(t_dp + mine + i, d);
+          ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            const float4 y = delta[(i + e) / 4];
+            const f2 z0 = mul2(pair_of(v + i + e), add2(pair_of(d + e), f2{y.x, y.y})),
+                     z1 = mul2(pair_of(v + i + e + 2), add2(pair_of(d + e + 2), f2{y.z, y.w}));
+            d[e] = __float_as_uint(z0.x);
+            d[e + 1] = __float_as_uint(z0.y);
+            d[e + 2] = __float_as_uint(z1.x);
+            d[e + 3] = __float_as_uint(z1.y);
+          }
+          if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (i + e < lo || i + e > hi) d[e] = 0;
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[e] = pack2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+          st16(t_dp + mine + i / 2, p);
+        }
+        st_wait();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&ctl.ds_full);
+          mbar_arrive(&ctl.t_empty[slot]);
+        }
       }
-      st_wait();
-      fence_before_sync();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&ctl.ds_full);
-        mbar_arrive(&ctl.t_empty[slot]);
-      }
-    }
-    if (ok && cnt > 0) ok = all_sync(mbar_wait(&ctl.o_full, 0, abort_flag));
-    if (ok) {
+      if (ok && cnt > 0) ok = all_sync(mbar_wait(&ctl.o_full, nu++ & 1, abort_flag));
+      if (!ok) break;
       fence_after_sync();
-      const bool mine = key < kt.n && (kt.kind != LOCAL || key % s.R != 0);
-      const size_t row = (size_t)kt.row0 + (size_t)key * kt.step;
-      bf16 *ok_ = (bf16*)a.dk + row * a.lddk + (size_t)hk * D, *ov = (bf16*)a.dv + row * a.lddv + (size_t)hk * D;
+      const bool in = key < u.n;
+      const size_t row = (size_t)u.row0 + (size_t)key * u.step;
+      bf16 *out_k = (bf16*)a.dk + row * a.lddk + (size_t)u.hk * D, *out_v = (bf16*)a.dv + row * a.lddv + (size_t)u.hk * D;
+      float* part = t.part_o + ((size_t)u.slot * 2 * kT + key) * D;
       float odd = 0.f;
 #pragma unroll
-      for (int j = half * (D / 2); j < (half + 1) * (D / 2); j += 32) {
-        uint32_t x[32], z[32];
+      for (int j0 = 0; j0 < D; j0 += 32) {     // D / 2 columns of dk, then of dv
+        const int j = half * (D / 2) + j0 % (D / 2);
+        const bool is_k = j0 < D / 2;
+        uint32_t x[32];
         float y[32];
         if (cnt > 0) {
-          ld32(t_dk + lanes + j, x);
-          ld32(t_dv + lanes + j, z);
+          ld32((is_k ? t_dk : t_dv) + lanes + j, x);
           ld_wait();
         } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) x[e] = z[e] = 0;
+          for (int e = 0; e < 32; ++e) x[e] = 0;
+        }
+        if (j0 + 32 == D && cnt > 0) {
+          fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctl.o_empty);
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
           odd = fmaf(__uint_as_float(x[e]), 0.f, odd);
-          odd = fmaf(__uint_as_float(z[e]), 0.f, odd);
-          y[e] = __uint_as_float(x[e]) * a.scale;
+          y[e] = __uint_as_float(x[e]) * (is_k ? a.scale : 1.f);
         }
-        if (mine) store_bf16<32>(ok_ + j, y);
+        if (in) {
+          if (u.parts == 1) {
+            store_bf16<32>((is_k ? out_k : out_v) + j, y);
+          } else {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(z[e]);
-        if (mine) store_bf16<32>(ov + j, y);
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<float4*>(part + (is_k ? 0 : kT * D) + j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+          }
+        }
       }
-      const unsigned bad = __ballot_sync(0xffffffffu, mine && odd != 0.f);
-      if (lane == 0 && bad) atomicOr(&s_bad[q], bad);
-    }
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    if (ok) {
-      unsigned todo = half == 0 ? s_bad[q] : 0u;
-      for (; todo; todo &= todo - 1) dkv_row<D>(s, a, kt, b, hk, 32 * q + __ffs(todo) - 1);
+      unsigned bad = __ballot_sync(0xffffffffu, in && odd != 0.f);
+      __syncwarp();
+      for (; bad; bad &= bad - 1) dkv_row<D>(s, a, t, u, 32 * q + __ffs(bad) - 1, half);
     }
     fence_before_sync();
   }
   finish(tid, warp, abort_flag, a.status, tmem, 512);
 }
 
+// Adds the parts of the key tiles that have several: a block per (tile, key head, 16 rows), a warp per row at a time.
+template <int D>
+__global__ void __launch_bounds__(256) k_gat_dkv_join(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a,
+                                                      const __grid_constant__ TcArgs t) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const KeyWork u(s, a, t, blockIdx.x * t.parts);
+  if (u.parts < 2) return;
+  const int lane = threadIdx.x & 31;
+  for (int i = 16 * blockIdx.y + (threadIdx.x >> 5); i < min(u.n, 16 * (int)blockIdx.y + 16); i += 8) {
+    const float* part = t.part_o + ((size_t)u.slot * 2 * kT + i) * D + (D / 32) * lane;
+    const size_t row = (size_t)u.row0 + (size_t)i * u.step;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      float x[D / 32];
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) x[e] = 0.f;
+      for (int p = 0; p < u.parts; ++p)
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) x[e] += part[((size_t)p * 2 + kv) * kT * D + e];
+      chan_store<D / 32>((kv ? (bf16*)a.dv + row * a.lddv : (bf16*)a.dk + row * a.lddk) + (size_t)u.hk * D + (D / 32) * lane, x);
+    }
+  }
+}
+
 // ---- host ------------------------------------------------------------------------------------------------
-int query_tiles(Seqs& s) {
+// Units of query tiles, nt at a time.
+int query_tiles(Seqs& s, int nt) {
   s.tile0[0] = 0;
-  for (int b = 0; b < s.B; ++b) s.tile0[b + 1] = s.tile0[b] + div_up(s.groups[b], groups_per_tile(kT, s.R));
+  for (int b = 0; b < s.B; ++b) s.tile0[b + 1] = s.tile0[b] + div_up(s.groups[b], nt * groups_per_tile(kT, s.R));
   return s.tile0[s.B];
 }
 int key_tiles(Seqs& s) {
   s.tile0[0] = 0;
-  for (int b = 0; b < s.B; ++b)
-    s.tile0[b + 1] = s.tile0[b] + div_up(s.ctx[b], kT) + div_up(s.groups[b], kT) + (s.R > 1 ? div_up(s.groups[b], groups_per_tile(kT, s.R)) : 0);
+  for (int b = 0; b < s.B; ++b) s.tile0[b + 1] = s.tile0[b] + div_up(s.ctx[b], kT) + div_up(s.groups[b], kT);
   return s.tile0[s.B];
 }
-// Key tiles of the longest query tile.
+// Key tiles of the longest query tile, steps of the key tile that most rows see.
 int most_keys(const Seqs& s) {
   int n = 0;
   for (int b = 0; b < s.B; ++b)
     if (s.groups[b]) n = std::max(n, div_up(s.ctx[b], kT) + div_up(s.groups[b], kT) + (s.R > 1));
   return n;
 }
+int most_steps(const Seqs& s, int per) {
+  int n = 0;
+  for (int b = 0; b < s.B; ++b) n = std::max(n, div_up(s.groups[b] * s.R, kT) * per);
+  return n;
+}
+// The sequences by length, the longest ones last or first: query tiles are dealt out from the last one's end (the longest
+// rows), key tiles from the first one's beginning (those that most rows see).
+Seqs sorted(const Seqs& s, bool longest_first) {
+  int at[PS_MAX_BATCH];
+  for (int b = 0; b < s.B; ++b) at[b] = b;
+  std::sort(at, at + s.B, [&](int x, int y) {
+    const int kx = div_up(s.ctx[x], kT) + div_up(s.groups[x], kT), ky = div_up(s.ctx[y], kT) + div_up(s.groups[y], kT);
+    return kx != ky ? (kx < ky) != longest_first : x < y;
+  });
+  Seqs r = s;
+  for (int b = 0; b < s.B; ++b) {
+    r.ctx[b] = s.ctx[at[b]]; r.groups[b] = s.groups[at[b]];
+    r.q0[b] = s.q0[at[b]]; r.kv0[b] = s.kv0[at[b]];
+  }
+  return r;
+}
 
 template <class Kern>
 cudaError_t ready(Kern kern, int smem, std::atomic<uint64_t>& done) { return allow_smem((const void*)kern, smem, done); }
 
 template <int D>
-cudaError_t forward(const Maps& maps, Seqs s, const AttnArgs& a, const TcArgs& t, cudaStream_t st) {
+cudaError_t forward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const TcArgs& t, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   if (cudaError_t e = ready(k_gat_fwd<D>, Fwd<D>::smem, done)) return e;
-  const int tiles = query_tiles(s);
-  cudaError_t e = launch_after(k_gat_fwd<D>, dim3((unsigned)tiles * a.n_heads, t.splits), dim3(Fwd<D>::threads), Fwd<D>::smem, st, true, maps, s, a, t);
+  Seqs s = sorted(s0, false);
+  const long long works = (long long)query_tiles(s, 2) * a.n_heads * t.splits;
+  cudaError_t e = launch_after(k_gat_fwd<D>, dim3((unsigned)std::min<long long>(works, device_sms())), dim3(Fwd<D>::threads),
+                               Fwd<D>::smem, st, true, maps, s, a, t);
   if (e != cudaSuccess || t.splits == 1) return e;
   const long long units = (long long)a.rows * a.n_heads;
   return launch_after(k_gat_join<D>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, true, a, t);
 }
 template <int D>
-cudaError_t backward(const Maps& maps, Seqs s, const AttnArgs& a, const TcArgs& t, cudaStream_t st) {
+cudaError_t backward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const TcArgs& tq, const TcArgs& tk, cudaStream_t st) {
   static std::atomic<uint64_t> done_q{0}, done_kv{0};
   if (cudaError_t e = ready(k_gat_dq<D>, Dq<D>::smem, done_q)) return e;
   if (cudaError_t e = ready(k_gat_dkv<D>, Dkv<D>::smem, done_kv)) return e;
   cudaError_t e = cudaSuccess;
-  if (const int tiles = query_tiles(s)) {
-    e = launch_after(k_gat_dq<D>, dim3((unsigned)tiles * a.n_heads, t.splits), dim3(Dq<D>::threads), Dq<D>::smem, st, true, maps, s, a, t);
-    if (e == cudaSuccess && t.splits > 1) {
+  const unsigned sms = device_sms();
+  if (a.rows > 0) {
+    const int groups = a.rows / s0.R;
+    // (more channels a lane mean fewer exchanges; registers hold as many rows as a group may have)
+    const auto blocks = [&](int C) { return dim3((unsigned)(((long long)groups * a.n_kv * (D / C) + 127) / 128)); };
+    if (s0.R == 1) e = launch_after(k_gat_masks<D, 1, 8>, blocks(8), dim3(128), 0, st, true, s0, a, groups);
+    else if (s0.R <= 5) e = launch_after(k_gat_masks<D, 5, 8>, blocks(8), dim3(128), 0, st, true, s0, a, groups);
+    else if (s0.R <= 9) e = launch_after(k_gat_masks<D, 9, 4>, blocks(4), dim3(128), 0, st, true, s0, a, groups);
+    else e = launch_after(k_gat_masks<D, 16, D / 32>, blocks(D / 32), dim3(128), 0, st, true, s0, a, groups);
+    if (e != cudaSuccess) return e;
+    Seqs s = sorted(s0, false);
+    const long long works = (long long)query_tiles(s, 1) * a.n_heads * tq.splits;
+    e = launch_after(k_gat_dq<D>, dim3((unsigned)std::min<long long>(works, sms)), dim3(Dq<D>::threads), Dq<D>::smem, st, true, maps,
+                     s, a, tq);
+    if (e == cudaSuccess && tq.splits > 1) {
       const long long units = (long long)a.rows * a.n_heads;
-      e = launch_after(k_gat_dq_join<D>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, true, a, t);
+      e = launch_after(k_gat_dq_join<D>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, true, a, tq);
     }
     if (e != cudaSuccess) return e;
   }
-  const int tiles = key_tiles(s);
-  return launch_after(k_gat_dkv<D>, dim3((unsigned)tiles * a.n_kv), dim3(Dkv<D>::threads), Dkv<D>::smem, st, true, maps, s, a);
+  Seqs s = sorted(s0, true);
+  const long long tiles = key_tiles(s), works = tiles * a.n_kv * tk.parts;
+  e = launch_after(k_gat_dkv<D>, dim3((unsigned)std::min<long long>(works, sms)), dim3(Dkv<D>::threads), Dkv<D>::smem, st, true, maps, s, a, tk);
+  if (e != cudaSuccess || tk.parts == 1) return e;
+  return launch_after(k_gat_dkv_join<D>, dim3((unsigned)(tiles * a.n_kv), kT / 16), dim3(256), 0, st, true, s, a, tk);
 }
 
 }  // namespace
 
 // Parts that a query tile's keys are dealt to, so that few query tiles still fill the device: as many as find room at
-// once (two blocks an SM forward, one backward), none with less than two key tiles.
+// once (a block an SM), none with less than two key tiles.
 int attn_splits(const Seqs& s, int n_heads, bool backward) {
   Seqs c = s;
-  const int blocks = query_tiles(c) * n_heads, room = device_sms() * (backward ? 1 : 2), most = most_keys(s) / 2;
-  if (blocks == 0) return 1;
-  return std::max(1, std::min(std::min(room / blocks, most), 32));
+  const long long units = (long long)query_tiles(c, backward ? 1 : 2) * n_heads;
+  if (units == 0) return 1;
+  return std::max(1, (int)std::min<long long>(std::min<long long>(device_sms() / units, most_keys(s) / 2), 32));
+}
+// Parts that a key tile's steps are dealt to, at most kParts: four units of work an SM, so that the last ones end at about
+// the same time although the first tiles of a sequence are seen by the most rows.
+void attn_parts(const Seqs& s, int n_kv, int per, TcArgs* t) {
+  constexpr int kParts = 8;
+  Seqs c = s;
+  const long long units = (long long)key_tiles(c) * n_kv;
+  const int steps = most_steps(s, per);
+  t->parts = units == 0 ? 1 : (int)std::max<long long>(1, std::min<long long>(std::min<long long>(kParts, 4ll * device_sms() / units), steps / 4));
+  t->cap = std::max(1, div_up(steps, t->parts));
+  t->key_units = units * t->parts;
 }
 
 bool attn_tc_takes(const AttnArgs& a, bool backward) {
   auto fits = [](const void* p, size_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld < (1ull << 36); };
-  if (!(a.scale >= 0.f)) return false;
+  if (!(a.scale > 0.f)) return false;
   if (!fits(a.q, a.ldq) || !fits(a.k, a.ldk) || !fits(a.v, a.ldv) || !fits(a.out, a.ldo)) return false;
   return !backward || (fits(a.dout, a.lddo) && fits(a.dq, a.lddq) && fits(a.dk, a.lddk) && fits(a.dv, a.lddv));
 }
 
-cudaError_t attn_tc(int D, bool backward_, const Seqs& s, const AttnArgs& a, const TcArgs& t, cudaStream_t st) {
+cudaError_t attn_tc(int D, bool backward_, const Seqs& s, const AttnArgs& a, const TcArgs& t, const TcArgs& tk, cudaStream_t st) {
   Maps m = {};
   const size_t wq = (size_t)a.n_heads * D, wk = (size_t)a.n_kv * D, keys = s.kv0[s.B];
   bool ok = make_rows_map(&m.q, a.q, a.rows, wq, a.ldq, 1) && make_rows_map(&m.k, a.k, keys, wk, a.ldk, 1) &&
@@ -1118,7 +1558,7 @@ cudaError_t attn_tc(int D, bool backward_, const Seqs& s, const AttnArgs& a, con
     ok = make_rows_map(&m.ks, a.k, keys, wk, a.ldk, s.R) && make_rows_map(&m.vs, a.v, keys, wk, a.ldv, s.R);
   if (ok && backward_) ok = make_rows_map(&m.dout, a.dout, a.rows, wq, a.lddo, 1);
   if (!ok) return cudaErrorNotSupported;
-  if (backward_) return D == 64 ? backward<64>(m, s, a, t, st) : backward<128>(m, s, a, t, st);
+  if (backward_) return D == 64 ? backward<64>(m, s, a, t, tk, st) : backward<128>(m, s, a, t, tk, st);
   return D == 64 ? forward<64>(m, s, a, t, st) : forward<128>(m, s, a, t, st);
 }
 

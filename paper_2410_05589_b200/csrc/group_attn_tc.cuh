@@ -9,8 +9,11 @@ struct Maps {
   CUtensorMap q, k, v, ks, vs, dout;   // ks, vs: rows of a group side by side (keys of the second kind)
 };
 struct TcArgs {
+  int gpt;            // groups of a query tile
   int splits;         // parts that a query tile's keys are dealt to
-  float* part_o;      // [splits][n_heads][rows][D] their outputs (forward) or dq
+  int parts, cap;     // parts that a key tile's steps are dealt to, steps of a part
+  long long key_units;   // key tiles times key heads times parts
+  float* part_o;      // [splits][n_heads][rows][D] their outputs (forward) or dq; [key units][dk, dv][128][D]
   float* part_l;      // [splits][n_heads][rows] their log-sum-exps
 };
 
@@ -18,10 +21,12 @@ struct TcArgs {
 // (tensor_map.cu).
 bool make_rows_map(CUtensorMap* m, const void* base, size_t rows, size_t cols, size_t ld, int R);
 int attn_splits(const Seqs& s, int n_heads, bool backward);
+void attn_parts(const Seqs& s, int n_kv, int per, TcArgs* t);
 // Whether the tensor maps and vector stores take these pointers and strides (and the softmax its scale: a
 // maximum of scores is one of scaled scores).
 bool attn_tc_takes(const AttnArgs& a, bool backward);
-cudaError_t attn_tc(int D, bool backward, const Seqs& s, const AttnArgs& a, const TcArgs& t, cudaStream_t st);
+cudaError_t attn_tc(int D, bool backward, const Seqs& s, const AttnArgs& a, const TcArgs& t, const TcArgs& tk,
+                    cudaStream_t st);   // tk: of the key tiles (backward)
 
 }  // namespace train
 }  // namespace ps
