@@ -70,6 +70,17 @@ __device__ __forceinline__ void ld32(uint32_t taddr, uint32_t* r) {
       : "r"(taddr)
       : "memory");
 }
+__device__ __forceinline__ void ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+template <int N>
+__device__ __forceinline__ void ldn(uint32_t taddr, uint32_t* r) {
+  if constexpr (N == 32) ld32(taddr, r); else ld16(taddr, r);
+}
 __device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::
@@ -151,12 +162,38 @@ __device__ __forceinline__ void mma_scores(uint32_t d, uint64_t a, uint64_t b) {
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) umma::mma_f16(d, a + step_k(ks), b + step_k(ks), idesc(kT, false), ks > 0);
 }
-// d (+)= A B over 128 rows, A (bf16) in tensor memory: its columns 0..63 and 64..127 at `half` columns' distance.
-template <int D>
-__device__ __forceinline__ void mma_sums(uint32_t d, uint32_t a, int half, uint64_t b, bool add) {
+// d (+)= A B over 128 rows, A (bf16) in tensor memory: the columns of W rows lie together, at W columns' distance (a thread
+// stores what it forms of W fp32 columns in the first half of the same).
+template <int D, int W>
+__device__ __forceinline__ void mma_sums(uint32_t d, uint32_t a, uint64_t b, bool add) {
 #pragma unroll
   for (int ks = 0; ks < kT / 16; ++ks)
-    mma_ts(d, a + (ks >> 2) * half + (ks & 3) * 8, b + step_mn(ks), idesc(D, true), add || ks > 0);
+    mma_ts(d, a + ks * 16 / W * W + ks * 16 % W / 2, b + step_mn(ks), idesc(D, true), add || ks > 0);
+}
+
+// What the rows of a warp see of columns j .. j + 31.
+enum { kNone, kSome, kAll };
+__device__ __forceinline__ int chunk_sees(int j, int lo, int hi) {
+  if (all_sync(lo <= j && hi >= j + 31)) return kAll;
+  return all_sync(hi < j || lo > j + 31) ? kNone : kSome;
+}
+// One bit for each of them that this row sees.
+__device__ __forceinline__ uint32_t seen_bits(int j, int lo, int hi) {
+  const uint32_t below = hi < j ? 0u : (hi >= j + 31 ? ~0u : (2u << (hi - j)) - 1);
+  return lo <= j ? below : (lo > j + 31 ? 0u : below & (~0u << (lo - j)));
+}
+// Their scores: -inf where it does not; products with them: zero.
+__device__ __forceinline__ void mask_scores(uint32_t* w, int j, int lo, int hi) {
+  const uint32_t bits = seen_bits(j, lo, hi);
+#pragma unroll
+  for (int e = 0; e < 32; ++e)
+    if (!(bits & (1u << e))) w[e] = 0xFF800000u;
+}
+__device__ __forceinline__ void mask_zero(uint32_t* w, int j, int lo, int hi) {
+  const uint32_t bits = seen_bits(j, lo, hi);
+#pragma unroll
+  for (int e = 0; e < 32; ++e)
+    if (!(bits & (1u << e))) w[e] = 0;
 }
 
 // ---- tiles ------------------------------------------------------------------------------------------
@@ -278,6 +315,12 @@ __device__ __forceinline__ float lane_dot(const float (&x)[D / 32], const float 
   return warp_sum(s);
 }
 
+// Unit of a persistent block's round: every other round backwards, so that no block has the longest unit of each.
+__device__ __forceinline__ int unit_of(int round) {
+  const int g = gridDim.x, b = blockIdx.x;
+  return round * g + (round & 1 ? g - 1 - b : b);
+}
+
 // The tail of a kernel whose waits are bounded: see umma_gemm.cuh.
 __device__ __forceinline__ void finish(int tid, int warp, volatile int* abort_flag, int* status, uint32_t tmem, int cols) {
   __syncthreads();
@@ -298,14 +341,16 @@ __device__ __forceinline__ void alloc_tmem(uint32_t* where, int cols) {
 
 // ---- forward ----------------------------------------------------------------------------------------
 // A persistent block an SM; a unit of its work are two neighbouring query tiles of a head, which share the key tiles
-// that pass through the ring.  Warp 0 issues the TMA loads, warp 1 the MMAs, four warps per query tile own a row a
-// thread.  The queue of the tensor cores is O0 += P0 V, S0 of the next keys, O1 += P1 V, S1 of the next keys (P lies in
+// that pass through the ring.  Warp 0 issues the TMA loads, warp 1 the MMAs; eight warps per query tile, two threads a
+// row with half of the keys each, which tell each other their maxima (what bounds a step is the latency of its instructions: with
+// one thread a row a step took twice as long).  The queue of the tensor cores is O0 += P0 V, S0 of the next keys, O1 += P1 V, S1 of the next keys (P lies in
 // S's columns: they work in order), so that one tile's softmax runs beside the other's products.
 template <int D>
 struct Fwd {
-  static constexpr int NS = D == 128 ? 5 : 10;
-  static constexpr int threads = 320;
-  static constexpr int smem = (2 + NS) * kTileBytes<D> + 2048;
+  static constexpr int NS = D == 128 ? 5 : 10;   // of the ring
+  static constexpr int threads = 576;
+  static constexpr int row_bytes = 2048;       // what the two warps of a row tell each other
+  static constexpr int smem = (2 + NS) * kTileBytes<D> + row_bytes + 1024;
 };
 struct FwdCtl {
   uint64_t full[10], empty[10], q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_empty[2];
@@ -313,9 +358,9 @@ struct FwdCtl {
   int abort_flag;
 };
 
-// Row r of query tile x over its key tiles [i0, i1), by one warp and over the keys it sees alone.
+// Half of the columns of row r of query tile x over its key tiles [i0, i1), by one warp and over the keys it sees alone.
 template <int D>
-__device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const QueryWork<2> u, int x, int r) {
+__device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const QueryWork<2> u, int x, int r, int half) {
   const int lane = threadIdx.x & 31, h = u.h;
   const size_t row_q = (size_t)u.qrow(x) + r;
   const TileRow tr(r, u.w.R);
@@ -351,13 +396,15 @@ __device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const Q
   if (t.splits == 1) {
     bf16* dst = (bf16*)a.out + row_q * a.ldo + (size_t)h * D;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * inv);
-    if (lane == 0) a.lse[(size_t)h * a.rows + row_q] = lse;
+    for (int e = 0; e < D / 32; ++e)
+      if (e / (D / 64) == half) dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * inv);
+    if (lane == 0 && half == 0) a.lse[(size_t)h * a.rows + row_q] = lse;
   } else {
     const size_t at = ((size_t)u.split * a.n_heads + h) * a.rows + row_q;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) t.part_o[at * D + lane + 32 * e] = o[e] * inv;
-    if (lane == 0) t.part_l[at] = lse;
+    for (int e = 0; e < D / 32; ++e)
+      if (e / (D / 64) == half) t.part_o[at * D + lane + 32 * e] = o[e] * inv;
+    if (lane == 0 && half == 0) t.part_l[at] = lse;
   }
 }
 
@@ -366,17 +413,23 @@ __global__ void __launch_bounds__(Fwd<D>::threads, 1)
 k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a,
           const __grid_constant__ TcArgs t) {
   using F = Fwd<D>;
-  extern __shared__ unsigned char smem_raw[];
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  // (no room for a shift to the tiles' boundary: shared memory begins on it, or the call fails)
+  if (base != raw) {
+    if (threadIdx.x == 0) atomicOr(a.status, kStatTimeout);
+    return;
+  }
   const uint32_t sq = base, ring = base + 2 * kTileBytes<D>;
-  FwdCtl& ctl = *reinterpret_cast<FwdCtl*>(smem_raw + (base - raw) + (2 + F::NS) * kTileBytes<D>);
+  unsigned char* s_row = smem_raw + (2 + F::NS) * kTileBytes<D>;
+  FwdCtl& ctl = *reinterpret_cast<FwdCtl*>(s_row + F::row_bytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < F::NS; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&ctl.q_full[i], 1); mbar_init(&ctl.q_empty[i], 1);
-      mbar_init(&ctl.s_full[i], 1); mbar_init(&ctl.p_full[i], 4);
-      mbar_init(&ctl.o_full[i], 1); mbar_init(&ctl.o_empty[i], 4);
+      mbar_init(&ctl.s_full[i], 1); mbar_init(&ctl.p_full[i], 8);
+      mbar_init(&ctl.o_full[i], 1); mbar_init(&ctl.o_empty[i], 8);
     }
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -406,7 +459,8 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
         ++it;
         return ok;
       };
-      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+        if (unit >= units) continue;
         const QueryWork<2> u(s, a, t, unit);
         if (u.i0 == u.i1) continue;
         for (int x = 0; ok && x < u.nt; ++x) {
@@ -435,7 +489,8 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
         fence_after_sync();
         return ring + it % F::NS * kTileBytes<D>;
       };
-      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+        if (unit >= units) continue;
         const QueryWork<2> u(s, a, t, unit);
         if (u.i0 == u.i1) continue;
         // S of query tile x with the key tile whose slots begin at `at`
@@ -462,7 +517,7 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
             if (ok && i == u.i0) ok = mbar_wait(&ctl.o_empty[x], (nq[x]++ & 1) ^ 1, abort_flag);
             if (!ok) break;
             fence_after_sync();
-            mma_sums<D>(t_o + x * kT, tmem + x * kT, 32, desc_mn(v), i > u.i0);
+            mma_sums<D, 64>(t_o + x * kT, tmem + x * kT, desc_mn(v), i > u.i0);
             if (own || x == u.nt - 1) mma_commit(&ctl.empty[vs % F::NS]);
             if (i == u.i1 - 1) mma_commit(&ctl.o_full[x]);
             else scores(i + 1, next, x);
@@ -472,44 +527,55 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
       }
     }
   } else {
-    const int q = warp & 3, r = 32 * q + lane, x = (warp - 2) >> 2;
-    const uint32_t lanes = (uint32_t)(32 * q) << 16, ts = tmem + x * kT + lanes, to = t_o + x * kT + lanes;
+    const int q = warp & 3, r = 32 * q + lane, x = (warp - 2) >> 3, half = ((warp - 2) >> 2) & 1;
+    const uint32_t lanes = (uint32_t)(32 * q) << 16, ts = tmem + x * kT + lanes + 64 * half, to = t_o + x * kT + lanes + half * (D / 2);
     const float c = a.scale * kLog2e;
     const TileRow tr(r, s.R);
+    // what the two warps of a row tell each other: maxima (two steps' worth, bf16), at the end their sums
+    unsigned char* own = s_row + (4 * x + q) * 256;
+    unsigned short* tops = reinterpret_cast<unsigned short*>(own);
+    float* sums = reinterpret_cast<float*>(own);
+    auto meet = [&] { asm volatile("bar.sync %0, 64;" ::"r"(1 + 4 * x + q) : "memory"); };
     int ns = 0, nu = 0;
-    bool ok = true;
-    for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+    // (a wait that gives up does not end the loop: the other warp of the row would wait for this one for good.  What is
+    // formed then is not used, and the waits that follow give up at once.)
+    for (int round = 0, unit; (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+      if (unit >= units) continue;
       const QueryWork<2> u(s, a, t, unit);
       if (x >= u.nt) continue;
       const int rows = u.rows(x), group = u.group(x);
       float m = -INFINITY, l = 0.f;
       for (int i = u.i0; i < u.i1; ++i, ++ns) {
+        mbar_wait(&ctl.s_full[x], ns & 1, abort_flag);
+        __syncwarp();
+        fence_after_sync();
+        uint32_t v[32];
+        ld32(ts, v);
         int x0, n, lo, hi;
         const int kind = u.w.tile(i, group, rows, x0, n);
         tr.sees(kind, x0, n, group, rows, lo, hi);
-        ok = all_sync(mbar_wait(&ctl.s_full[x], ns & 1, abort_flag));
-        if (!ok) break;
-        fence_after_sync();
-        uint32_t v[kT];
+        lo -= 64 * half;
+        hi -= 64 * half;
+        const bool whole = all_sync(lo <= 0 && hi >= 63);
+        // (the scores are read twice: 64 of them leave no registers for anything else)
+        float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < kT; j += 32) ld32(ts + j, v + j);
-        ld_wait();
-        if (!all_sync(hi >= kT - 1)) {
+        for (int j = 0; j < 64; j += 32) {
+          ld_wait();
+          const int see = whole ? kAll : chunk_sees(j, lo, hi);
+          if (see == kSome) mask_scores(v, j, lo, hi);
+          if (see != kNone) {
 #pragma unroll
-          for (int j = 0; j < kT; ++j)
-            if (j > hi) v[j] = 0xFF800000u;   // -inf
+            for (int k = 0; k < 32; k += 8)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) y[e] = max3(y[e], __uint_as_float(v[k + e]), __uint_as_float(v[k + 4 + e]));
+          }
+          ld32(ts + (j == 0 ? 32 : 0), v);   // (behind the second chunk: the first one again)
         }
-        if (!all_sync(lo <= 0)) {
-#pragma unroll
-          for (int j = 0; j < kT; ++j)
-            if (j < lo) v[j] = 0xFF800000u;
-        }
-        float y[4] = {m, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int j = 0; j < kT; j += 8)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = max3(y[e], __uint_as_float(v[j + e]), __uint_as_float(v[j + 4 + e]));
-        const float top = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+        const unsigned short mine = __bfloat16_as_ushort(__float2bfloat16_ru(fmaxf(max3(y[0], y[1], y[2]), y[3])));
+        tops[(2 * (ns & 1) + half) * 32 + lane] = mine;
+        meet();
+        const float top = fmaxf(__uint_as_float((uint32_t)mine << 16), __uint_as_float((uint32_t)tops[(2 * (ns & 1) + 1 - half) * 32 + lane] << 16));
         if (i == u.i0) {
           m = top;
         } else {
@@ -521,7 +587,7 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
             l *= f;
             if (grown) m = top;
 #pragma unroll 1
-            for (int j = 0; j < D; j += 32) {
+            for (int j = 0; j < D / 2; j += 32) {
               uint32_t o[32];
               ld32(to + j, o);
               ld_wait();
@@ -534,14 +600,23 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
         const float ref = m > -INFINITY ? m * c : 0.f;
         f2 sum = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < kT; j += 32) {
+        for (int j = 0; j < 64; j += 32) {
           uint32_t p[16];
+          ld_wait();
+          const int see = whole ? kAll : chunk_sees(j, lo, hi);
+          if (see == kNone) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            const f2 z = fma2(pair_of(v + j + e), f2{c, c}, f2{-ref, -ref}), w = {ex2(z.x), ex2(z.y)};
-            sum = add2(sum, w);
-            p[e / 2] = pack2(w.x, w.y);
+            for (int e = 0; e < 16; ++e) p[e] = 0;
+          } else {
+            if (see == kSome) mask_scores(v, j, lo, hi);
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const f2 z = fma2(pair_of(v + e), f2{c, c}, f2{-ref, -ref}), w = {ex2(z.x), ex2(z.y)};
+              sum = add2(sum, w);
+              p[e / 2] = pack2(w.x, w.y);
+            }
           }
+          if (j == 0) ld32(ts + 32, v);
           st16(ts + j / 2, p);
         }
         l += sum.x + sum.y;
@@ -550,15 +625,20 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
         __syncwarp();
         if (lane == 0) mbar_arrive(&ctl.p_full[x]);
       }
-      if (ok && u.i0 < u.i1) ok = all_sync(mbar_wait(&ctl.o_full[x], nu++ & 1, abort_flag));
-      if (!ok) break;
+      meet();
+      sums[32 * half + lane] = l;
+      meet();
+      l += sums[32 * (1 - half) + lane];
+      meet();
+      if (u.i0 < u.i1) mbar_wait(&ctl.o_full[x], nu++ & 1, abort_flag);
+      __syncwarp();
       fence_after_sync();
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const size_t row = (size_t)u.qrow(x) + r, at = ((size_t)u.split * a.n_heads + u.h) * a.rows + row;
-      bf16* dst = (bf16*)a.out + row * a.ldo + (size_t)u.h * D;
+      bf16* dst = (bf16*)a.out + row * a.ldo + (size_t)u.h * D + half * (D / 2);
       float odd = l * 0.f;                   // no number once a sum is not finite
 #pragma unroll
-      for (int j = 0; j < D; j += 32) {
+      for (int j = 0; j < D / 2; j += 32) {
         uint32_t o[32];
         float y[32];
         if (u.i0 < u.i1) {
@@ -568,7 +648,7 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0;
         }
-        if (j + 32 == D && u.i0 < u.i1) {    // read back: the next unit's products may overwrite it
+        if (j + 32 == D / 2 && u.i0 < u.i1) {    // read back: the next unit's products may overwrite it
           fence_before_sync();
           __syncwarp();
           if (lane == 0) mbar_arrive(&ctl.o_empty[x]);
@@ -584,18 +664,18 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
           } else {
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(t.part_o + at * D + j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+              *reinterpret_cast<float4*>(t.part_o + at * D + half * (D / 2) + j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
           }
         }
       }
-      if (r < rows) {
+      if (r < rows && half == 0) {
         const float lse = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
         if (t.splits == 1) a.lse[(size_t)u.h * a.rows + row] = lse;
         else t.part_l[at] = lse;
       }
       unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f);
       __syncwarp();
-      for (; bad; bad &= bad - 1) fwd_row<D>(a, t, u, x, 32 * q + __ffs(bad) - 1);
+      for (; bad; bad &= bad - 1) fwd_row<D>(a, t, u, x, 32 * q + __ffs(bad) - 1, half);
     }
     fence_before_sync();
   }
@@ -632,13 +712,13 @@ __global__ void __launch_bounds__(256) k_gat_join(const __grid_constant__ AttnAr
 }
 
 // ---- backward: dq -------------------------------------------------------------------------------------
-// A persistent block an SM, one query tile of a head at a time.  Two groups of four warps share a tile's rows, half of the
-// keys each.  The scores pass through registers, so that the next tile's are formed as soon as they are read; dP has
-// two buffers, and dS takes dP's columns (each half its own): the tensor cores work on S, dP of the next tile and dQ of the
+// A persistent block an SM, one query tile of a head at a time.  Four groups of four warps share a tile's rows, a quarter of
+// the keys each.  The scores pass through registers, so that the next tile's are formed as soon as they are read; dP has
+// two buffers, and dS takes dP's columns (each quarter its own): the tensor cores work on S, dP of the next tile and dQ of the
 // last one while the warps turn this one's into dS.
 template <int D>
 struct Dq {
-  static constexpr int NK = 3, NV = 2, threads = 320;
+  static constexpr int NK = 3, NV = 2, threads = 576;
   static constexpr int smem = (2 + NK + NV) * kTileBytes<D> + 2048;
 };
 struct DqCtl {
@@ -647,9 +727,9 @@ struct DqCtl {
   int abort_flag;
 };
 
-// Columns [half D/2, ..) of row r of the query tile, by one warp and over the keys the row sees alone.
+// A quarter of the columns of row r of the query tile, by one warp and over the keys the row sees alone.
 template <int D>
-__device__ __noinline__ void dq_row(const AttnArgs& a, const TcArgs& t, const QueryWork<1> u, int r, int half) {
+__device__ __noinline__ void dq_row(const AttnArgs& a, const TcArgs& t, const QueryWork<1> u, int r, int quarter) {
   const int lane = threadIdx.x & 31, h = u.h;
   const size_t row_q = (size_t)u.qrow(0) + r;
   const TileRow tr(r, u.w.R);
@@ -678,7 +758,7 @@ __device__ __noinline__ void dq_row(const AttnArgs& a, const TcArgs& t, const Qu
   bf16* dst = (bf16*)a.dq + row_q * a.lddq + (size_t)h * D;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) {
-    if (e / (D / 64) != half) continue;
+    if ((lane + 32 * e) / (D / 4) != quarter) continue;
     if (t.splits > 1) part[lane + 32 * e] = o[e] * a.scale;
     else dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * a.scale);
   }
@@ -689,7 +769,7 @@ __global__ void __launch_bounds__(Dq<D>::threads, 1)
 k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a,
          const __grid_constant__ TcArgs t) {
   using F = Dq<D>;
-  extern __shared__ unsigned char smem_raw[];
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t sq = base, so = sq + kTileBytes<D>, sk = so + kTileBytes<D>, sv = sk + F::NK * kTileBytes<D>;
   DqCtl& ctl = *reinterpret_cast<DqCtl*>(smem_raw + (base - raw) + (2 + F::NK + F::NV) * kTileBytes<D>);
@@ -700,12 +780,12 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
     mbar_init(&ctl.q_full, 2);
     mbar_init(&ctl.q_empty, 1);
     mbar_init(&ctl.s_full, 1);
-    mbar_init(&ctl.s_empty, 8);
+    mbar_init(&ctl.s_empty, 16);
     mbar_init(&ctl.dp_full[0], 1);
     mbar_init(&ctl.dp_full[1], 1);
-    mbar_init(&ctl.ds_full, 8);
+    mbar_init(&ctl.ds_full, 16);
     mbar_init(&ctl.o_full, 1);
-    mbar_init(&ctl.o_empty, 8);
+    mbar_init(&ctl.o_empty, 16);
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
@@ -726,7 +806,8 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
     if (lane == 0) {
       int it = 0, nu = 0;
       bool ok = true;
-      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+        if (unit >= units) continue;
         const QueryWork<1> u(s, a, t, unit);
         if (u.i0 == u.i1) continue;
         ok = mbar_wait(&ctl.q_empty, (nu++ & 1) ^ 1, abort_flag);
@@ -766,7 +847,8 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
         mma_commit(&ctl.v_empty[vs]);
         if (last) mma_commit(&ctl.q_empty);
       };
-      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+        if (unit >= units) continue;
         const QueryWork<1> u(s, a, t, unit);
         const int cnt = u.i1 - u.i0;
         if (cnt == 0) continue;
@@ -779,7 +861,7 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
           if (!ok) break;
           fence_after_sync();
           const int ks = it % F::NK;
-          mma_sums<D>(t_o, t_dp + (it & 1) * kT, 64, desc_mn(sk + ks * kTileBytes<D>), i > 0);
+          mma_sums<D, 32>(t_o, t_dp + (it & 1) * kT, desc_mn(sk + ks * kTileBytes<D>), i > 0);
           mma_commit(&ctl.k_empty[ks]);
           if (i + 1 == cnt) mma_commit(&ctl.o_full);
         }
@@ -787,64 +869,56 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
       }
     }
   } else {
-    const int q = warp & 3, half = (warp - 2) >> 2, r = 32 * q + lane;
-    const uint32_t lanes = (uint32_t)(32 * q) << 16, mine = lanes + 64 * half;
+    const int q = warp & 3, quarter = (warp - 2) >> 2, r = 32 * q + lane;
+    const uint32_t lanes = (uint32_t)(32 * q) << 16, mine = lanes + 32 * quarter;
     const float c = a.scale * kLog2e;
     const TileRow tr(r, s.R);
     int it = 0, nu = 0;
     bool ok = true;
-    for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+    for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+      if (unit >= units) continue;
       const QueryWork<1> u(s, a, t, unit);
       const int rows = u.rows(0), cnt = u.i1 - u.i0;
       const size_t row = (size_t)u.qrow(0) + r, at = (size_t)u.h * a.rows + row;
       const float lse = r < rows ? a.lse[at] * kLog2e : 0.f, delta = r < rows ? a.delta[at] : 0.f;
       for (int i = u.i0; i < u.i1; ++i, ++it) {
-        int x0, n, lo, hi;
-        const int kind = u.w.tile(i, u.group(0), rows, x0, n);
-        tr.sees(kind, x0, n, u.group(0), rows, lo, hi);
-        lo -= 64 * half;
-        hi -= 64 * half;
         ok = all_sync(mbar_wait(&ctl.s_full, it & 1, abort_flag));
         if (!ok) break;
         fence_after_sync();
-        uint32_t v[64];
+        uint32_t v[32], d[32], p[16];
         ld32(tmem + mine, v);
-        ld32(tmem + mine + 32, v + 32);
+        int x0, n, lo, hi;
+        const int kind = u.w.tile(i, u.group(0), rows, x0, n);
+        tr.sees(kind, x0, n, u.group(0), rows, lo, hi);
+        lo -= 32 * quarter;
+        hi -= 32 * quarter;
+        const bool whole = all_sync(lo <= 0 && hi >= 31);
         ld_wait();
         fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(&ctl.s_empty);
 #pragma unroll
-        for (int j = 0; j < 64; j += 2) {
+        for (int j = 0; j < 32; j += 2) {
           const f2 z = fma2(pair_of(v + j), f2{c, c}, f2{-lse, -lse});
           v[j] = __float_as_uint(ex2(z.x));
           v[j + 1] = __float_as_uint(ex2(z.y));
         }
-        const bool whole = all_sync(lo <= 0 && hi >= 63);
         const uint32_t td = t_dp + (it & 1) * kT + mine;
         ok = all_sync(mbar_wait(&ctl.dp_full[it & 1], (it >> 1) & 1, abort_flag));
         if (!ok) break;
         fence_after_sync();
+        ld32(td, d);
+        ld_wait();
 #pragma unroll
-        for (int j = 0; j < 64; j += 32) {
-          uint32_t d[32], p[16];
-          ld32(td + j, d);
-          ld_wait();
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            const f2 z = mul2(pair_of(v + j + e), add2(pair_of(d + e), f2{-delta, -delta}));
-            d[e] = __float_as_uint(z.x);
-            d[e + 1] = __float_as_uint(z.y);
-          }
-          if (!whole) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (j + e < lo || j + e > hi) d[e] = 0;
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) p[e] = pack2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
-          st16(td + j / 2, p);
+        for (int e = 0; e < 32; e += 2) {
+          const f2 z = mul2(pair_of(v + e), add2(pair_of(d + e), f2{-delta, -delta}));
+          d[e] = __float_as_uint(z.x);
+          d[e + 1] = __float_as_uint(z.y);
         }
+        if (!whole) mask_zero(d, 0, lo, hi);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] = pack2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+        st16(td, p);
         st_wait();
         fence_before_sync();
         __syncwarp();
@@ -853,44 +927,37 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
       if (ok && cnt > 0) ok = all_sync(mbar_wait(&ctl.o_full, nu++ & 1, abort_flag));
       if (!ok) break;
       fence_after_sync();
-      float* part = t.part_o + (((size_t)u.split * a.n_heads + u.h) * a.rows + row) * D;
-      bf16* dst = (bf16*)a.dq + row * a.lddq + (size_t)u.h * D;
-      float odd = 0.f;
+      constexpr int N = D / 4;
+      float* part = t.part_o + (((size_t)u.split * a.n_heads + u.h) * a.rows + row) * D + N * quarter;
+      bf16* dst = (bf16*)a.dq + row * a.lddq + (size_t)u.h * D + N * quarter;
+      float odd = 0.f, y[N];
+      uint32_t o[N];
+      if (cnt > 0) {
+        ldn<N>(t_o + lanes + N * quarter, o);
+        ld_wait();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.o_empty);
+      } else {
 #pragma unroll
-      for (int j0 = 0; j0 < D / 2; j0 += 32) {
-        const int j = half * (D / 2) + j0;
-        uint32_t o[32];
-        float y[32];
-        if (cnt > 0) {
-          ld32(t_o + lanes + j, o);
-          ld_wait();
+        for (int e = 0; e < N; ++e) o[e] = 0;
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        odd = fmaf(__uint_as_float(o[e]), 0.f, odd);
+        y[e] = __uint_as_float(o[e]) * a.scale;
+      }
+      if (r < rows) {
+        if (t.splits == 1) {
+          store_bf16<N>(dst, y);
         } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0;
-        }
-        if (j0 + 32 == D / 2 && cnt > 0) {
-          fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&ctl.o_empty);
-        }
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          odd = fmaf(__uint_as_float(o[e]), 0.f, odd);
-          y[e] = __uint_as_float(o[e]) * a.scale;
-        }
-        if (r < rows) {
-          if (t.splits == 1) {
-            store_bf16<32>(dst + j, y);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(part + j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
-          }
+          for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(part + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
         }
       }
       unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f);
       __syncwarp();
-      for (; bad; bad &= bad - 1) dq_row<D>(a, t, u, 32 * q + __ffs(bad) - 1, half);
+      for (; bad; bad &= bad - 1) dq_row<D>(a, t, u, 32 * q + __ffs(bad) - 1, quarter);
     }
     fence_before_sync();
   }
@@ -958,7 +1025,7 @@ __device__ __forceinline__ float chan_dot(const Chans<C>& x, const Chans<C>& y) 
 
 // D / C lanes per (group, key head); RM: most rows of a group that the registers hold.
 template <int D, int RM, int C>
-__global__ void __launch_bounds__(128, RM <= 9 ? 3 : 2) k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, int groups) {
+__global__ void __launch_bounds__(128, RM <= 5 ? 4 : (RM <= 9 ? 3 : 2)) k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, int groups) {
   constexpr int L = D / C;
   pdl_launch_dependents();
   pdl_wait();
@@ -1050,11 +1117,11 @@ __global__ void __launch_bounds__(128, RM <= 9 ? 3 : 2) k_gat_masks(const __grid
 // A persistent block an SM, one key tile (context or real rows) and key head at a time, or a part of its steps:
 // the query tiles of all heads that share the key head.  Tensor memory is full with S^T (P^T in its columns), dP^T (dS^T
 // in its columns), dK and dV.  The warps form P^T while the tensor cores work on dK and dP^T, and dS^T while they work on
-// dV and the next step's S^T.  A thread owns a key and half of the query columns, whose lse and delta a warp
-// of its own puts into shared memory.
+// dV and the next step's S^T.  A thread owns a key and a quarter of the query columns, whose lse and delta a
+// warp of its own puts into shared memory.
 template <int D>
 struct Dkv {
-  static constexpr int threads = 352;
+  static constexpr int threads = 608;
   static constexpr int smem = 6 * kTileBytes<D> + 1024 + 2 * 2 * kT * 4 + 1024;
 };
 struct DkvCtl {
@@ -1089,9 +1156,21 @@ struct KeyWork {
     if (t.parts == 1) { parts = 1; j0 = 0; j1 = cnt; }
   }
   __device__ bool there() const { return part < parts; }
-  // Query row (of the sequence) and head of step j.
-  __device__ int head(int j, int per) const { return hk * per + j / per_head; }
-  __device__ int row(int j) const { return q_begin + j % per_head * kT; }
+  // Walks the steps: head and first query row (of the sequence).
+  struct Step {
+    int h, r0, q_begin, q_end;
+    __device__ Step(const KeyWork& u, int per) {
+      const int hh = u.j0 / max(1, u.per_head);
+      h = u.hk * per + hh;
+      q_begin = u.q_begin;
+      q_end = u.q_end;
+      r0 = q_begin + (u.j0 - hh * u.per_head) * kT;
+    }
+    __device__ void next() {
+      r0 += kT;
+      if (r0 >= q_end) { r0 = q_begin; ++h; }
+    }
+  };
   // Query rows that see key i of the tile: [lo, hi].
   __device__ void seen(int i, int R, int& lo, int& hi) const {
     lo = kind == REAL ? (x0 + i) * R : 0;
@@ -1099,9 +1178,9 @@ struct KeyWork {
   }
 };
 
-// Columns [half D/2, ..) of dk and dv of key i of the tile, by one warp and over the rows that see it alone.
+// Quarter of the columns of dk and dv of key i of the tile, by one warp and over the rows that see it alone.
 template <int D>
-__device__ __noinline__ void dkv_row(const Seqs& s, const AttnArgs& a, const TcArgs& t, const KeyWork u, int i, int half) {
+__device__ __noinline__ void dkv_row(const Seqs& s, const AttnArgs& a, const TcArgs& t, const KeyWork u, int i, int quarter) {
   const int lane = threadIdx.x & 31;
   const size_t row = (size_t)u.row0 + (size_t)i * u.step;
   float k[D / 32], v[D / 32], dk[D / 32], dv[D / 32];
@@ -1111,19 +1190,20 @@ __device__ __noinline__ void dkv_row(const Seqs& s, const AttnArgs& a, const TcA
   for (int e = 0; e < D / 32; ++e) dk[e] = dv[e] = 0.f;
   int lo, hi;
   u.seen(i, s.R, lo, hi);
-  for (int j = u.j0; j < u.j1; ++j) {
-    const int h = u.head(j, a.per), r0 = u.row(j);
+  KeyWork::Step x(u, a.per);
+  for (int j = u.j0; j < u.j1; ++j, x.next()) {
+    const int h = x.h, r0 = x.r0;
     for (int r = max(lo, r0); r <= min(hi, r0 + kT - 1); ++r) {
       const size_t qr = (size_t)s.q0[u.b] + r;
-      float x[D / 32], g[D / 32];
-      lane_load<D>((const bf16*)a.q + qr * a.ldq + (size_t)h * D, lane, x);
+      float q[D / 32], g[D / 32];
+      lane_load<D>((const bf16*)a.q + qr * a.ldq + (size_t)h * D, lane, q);
       lane_load<D>((const bf16*)a.dout + qr * a.lddo + (size_t)h * D, lane, g);
-      const float p = exp2f((lane_dot<D>(x, k) * a.scale - a.lse[(size_t)h * a.rows + qr]) * kLog2e);
+      const float p = exp2f((lane_dot<D>(q, k) * a.scale - a.lse[(size_t)h * a.rows + qr]) * kLog2e);
       const float ds = p * (lane_dot<D>(g, v) - a.delta[(size_t)h * a.rows + qr]);
 #pragma unroll
       for (int e = 0; e < D / 32; ++e) {
         dv[e] = fmaf(p, g[e], dv[e]);
-        dk[e] = fmaf(ds, x[e], dk[e]);
+        dk[e] = fmaf(ds, q[e], dk[e]);
       }
     }
   }
@@ -1131,7 +1211,7 @@ __device__ __noinline__ void dkv_row(const Seqs& s, const AttnArgs& a, const TcA
   float* part = t.part_o + ((size_t)u.slot * 2 * kT + i) * D;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) {
-    if (e / (D / 64) != half) continue;
+    if ((lane + 32 * e) / (D / 4) != quarter) continue;
     if (u.parts > 1) {
       part[lane + 32 * e] = dk[e] * a.scale;
       part[kT * D + lane + 32 * e] = dv[e];
@@ -1146,7 +1226,7 @@ template <int D>
 __global__ void __launch_bounds__(Dkv<D>::threads, 1)
 k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a,
           const __grid_constant__ TcArgs t) {
-  extern __shared__ unsigned char smem_raw[];
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t sk = base, sv = sk + kTileBytes<D>, sq = sv + kTileBytes<D>, sg = sq + 2 * kTileBytes<D>;
   float* s_stat = reinterpret_cast<float*>(smem_raw + (base - raw) + 6 * kTileBytes<D>);   // [slot][-lse, -delta][128]
@@ -1156,16 +1236,16 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
     for (int i = 0; i < 2; ++i) {
       mbar_init(&ctl.q_full[i], 1); mbar_init(&ctl.q_empty[i], 1);
       mbar_init(&ctl.g_full[i], 1); mbar_init(&ctl.g_empty[i], 1);
-      mbar_init(&ctl.t_full[i], 32); mbar_init(&ctl.t_empty[i], 8);
+      mbar_init(&ctl.t_full[i], 32); mbar_init(&ctl.t_empty[i], 16);
     }
     mbar_init(&ctl.k_full, 2);
     mbar_init(&ctl.k_empty, 1);
     mbar_init(&ctl.s_full, 1);
-    mbar_init(&ctl.p_full, 8);
+    mbar_init(&ctl.p_full, 16);
     mbar_init(&ctl.dp_full, 1);
-    mbar_init(&ctl.ds_full, 8);
+    mbar_init(&ctl.ds_full, 16);
     mbar_init(&ctl.o_full, 1);
-    mbar_init(&ctl.o_empty, 8);
+    mbar_init(&ctl.o_empty, 16);
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
@@ -1186,7 +1266,8 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
     if (lane == 0) {
       int it = 0, nu = 0;
       bool ok = true;
-      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+        if (unit >= units) continue;
         const KeyWork u(s, a, t, unit);
         if (!u.there() || u.j0 == u.j1) continue;
         ok = mbar_wait(&ctl.k_empty, (nu++ & 1) ^ 1, abort_flag);
@@ -1194,8 +1275,9 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
         const int base_row = u.kind == CTX ? s.kv0[u.b] : s.kv0[u.b] + s.ctx[u.b];
         load_keys<D>(sk, &maps.k, &maps.ks, u.kind, base_row, s.R, u.x0, u.hk * D, &ctl.k_full);
         load_keys<D>(sv, &maps.v, &maps.vs, u.kind, base_row, s.R, u.x0, u.hk * D, &ctl.k_full);
-        for (int j = u.j0; j < u.j1; ++j, ++it) {
-          const int r0 = s.q0[u.b] + u.row(j), col = u.head(j, a.per) * D, slot = it & 1;
+        KeyWork::Step x(u, a.per);
+        for (int j = u.j0; j < u.j1; ++j, ++it, x.next()) {
+          const int r0 = s.q0[u.b] + x.r0, col = x.h * D, slot = it & 1;
           const uint32_t parity = ((it >> 1) & 1) ^ 1;
           ok = mbar_wait(&ctl.q_empty[slot], parity, abort_flag);
           if (!ok) break;
@@ -1225,7 +1307,8 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
         mma_commit(&ctl.dp_full);
         if (last) mma_commit(&ctl.k_empty);
       };
-      for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+        if (unit >= units) continue;
         const KeyWork u(s, a, t, unit);
         const int cnt = u.j1 - u.j0;
         if (!u.there() || cnt == 0) continue;
@@ -1237,13 +1320,13 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
           if (ok && i == 0) ok = mbar_wait(&ctl.o_empty, (nu & 1) ^ 1, abort_flag);
           if (!ok) break;
           fence_after_sync();
-          mma_sums<D>(t_dv, tmem, 64, desc_mn(sg + (it & 1) * kTileBytes<D>), i > 0);
+          mma_sums<D, 32>(t_dv, tmem, desc_mn(sg + (it & 1) * kTileBytes<D>), i > 0);
           mma_commit(&ctl.g_empty[it & 1]);
           if (i + 1 < cnt) scores(it + 1);
           ok = ok && mbar_wait(&ctl.ds_full, it & 1, abort_flag);
           if (!ok) break;
           fence_after_sync();
-          mma_sums<D>(t_dk, t_dp, 64, desc_mn(sq + (it & 1) * kTileBytes<D>), i > 0);
+          mma_sums<D, 32>(t_dk, t_dp, desc_mn(sq + (it & 1) * kTileBytes<D>), i > 0);
           mma_commit(&ctl.q_empty[it & 1]);
           if (i + 1 < cnt) dprob(it + 1, i + 2 == cnt);
           else mma_commit(&ctl.o_full);
@@ -1254,14 +1337,16 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
   } else if (warp == 2) {
     int it = 0;
     bool ok = true;
-    for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+    for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+      if (unit >= units) continue;
       const KeyWork u(s, a, t, unit);
       if (!u.there()) continue;
-      for (int j = u.j0; j < u.j1; ++j, ++it) {
-        const int r0 = u.row(j), slot = it & 1;
+      KeyWork::Step x(u, a.per);
+      for (int j = u.j0; j < u.j1; ++j, ++it, x.next()) {
+        const int r0 = x.r0, slot = it & 1;
         ok = all_sync(mbar_wait(&ctl.t_empty[slot], ((it >> 1) & 1) ^ 1, abort_flag));
         if (!ok) break;
-        const size_t at = (size_t)u.head(j, a.per) * a.rows + s.q0[u.b] + r0;
+        const size_t at = (size_t)x.h * a.rows + s.q0[u.b] + r0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int col = lane + 32 * e;
@@ -1273,31 +1358,32 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
       }
     }
   } else {
-    const int q = warp & 3, half = (warp - 3) >> 2, key = 32 * q + lane;
-    const uint32_t lanes = (uint32_t)(32 * q) << 16, mine = lanes + 64 * half;
+    const int q = warp & 3, quarter = (warp - 3) >> 2, key = 32 * q + lane;
+    const uint32_t lanes = (uint32_t)(32 * q) << 16, mine = lanes + 32 * quarter;
     const float c = a.scale * kLog2e;
     int it = 0, nu = 0;
     bool ok = true;
-    for (int unit = blockIdx.x; ok && unit < units; unit += gridDim.x) {
+    for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+      if (unit >= units) continue;
       const KeyWork u(s, a, t, unit);
       if (!u.there()) continue;
       const int cnt = u.j1 - u.j0;
       int see0, see1;
       u.seen(key, s.R, see0, see1);
-      for (int j = u.j0; j < u.j1; ++j, ++it) {
-        const int r0 = u.row(j) + 64 * half, slot = it & 1, lo = see0 - r0, hi = see1 - r0;
-        const bool whole = all_sync(lo <= 0 && hi >= 63);
-        const float4 *lse = reinterpret_cast<const float4*>(s_stat + (2 * slot) * kT + 64 * half),
-                     *delta = reinterpret_cast<const float4*>(s_stat + (2 * slot + 1) * kT + 64 * half);
+      KeyWork::Step x(u, a.per);
+      for (int j = u.j0; j < u.j1; ++j, ++it, x.next()) {
+        const int r0 = x.r0 + 32 * quarter, slot = it & 1, lo = see0 - r0, hi = see1 - r0;
+        const bool whole = all_sync(lo <= 0 && hi >= 31);
+        const float4 *lse = reinterpret_cast<const float4*>(s_stat + (2 * slot) * kT + 32 * quarter),
+                     *delta = reinterpret_cast<const float4*>(s_stat + (2 * slot + 1) * kT + 32 * quarter);
         ok = all_sync(mbar_wait(&ctl.t_full[slot], (it >> 1) & 1, abort_flag)) && all_sync(mbar_wait(&ctl.s_full, it & 1, abort_flag));
         if (!ok) break;
         fence_after_sync();
-        uint32_t v[64];
+        uint32_t v[32], d[32], p[16];
         ld32(tmem + mine, v);
-        ld32(tmem + mine + 32, v + 32);
         ld_wait();
 #pragma unroll
-        for (int i = 0; i < 64; i += 4) {
+        for (int i = 0; i < 32; i += 4) {
           const float4 y = lse[i / 4];
           const f2 z0 = fma2(pair_of(v + i), f2{c, c}, f2{y.x, y.y}), z1 = fma2(pair_of(v + i + 2), f2{c, c}, f2{y.z, y.w});
           v[i] = __float_as_uint(ex2(z0.x));
@@ -1305,17 +1391,10 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
           v[i + 2] = __float_as_uint(ex2(z1.x));
           v[i + 3] = __float_as_uint(ex2(z1.y));
         }
-        if (!whole) {
+        if (!whole) mask_zero(v, 0, lo, hi);
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (i < lo || i > hi) v[i] = 0;
-        }
-        {
-          uint32_t p[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) p[e] = pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
-          st32(tmem + mine, p);
-        }
+        for (int e = 0; e < 16; ++e) p[e] = pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+        st16(tmem + mine, p);
         st_wait();
         fence_before_sync();
         __syncwarp();
@@ -1323,30 +1402,22 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
         ok = all_sync(mbar_wait(&ctl.dp_full, it & 1, abort_flag));
         if (!ok) break;
         fence_after_sync();
+        ld32(t_dp + mine, d);
+        ld_wait();
 #pragma unroll
-        for (int i = 0; i < 64; i += 32) {
-          uint32_t d[32], p[16];
-          ld32(t_dp + mine + i, d);
-          ld_wait();
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            const float4 y = delta[(i + e) / 4];
-            const f2 z0 = mul2(pair_of(v + i + e), add2(pair_of(d + e), f2{y.x, y.y})),
-                     z1 = mul2(pair_of(v + i + e + 2), add2(pair_of(d + e + 2), f2{y.z, y.w}));
-            d[e] = __float_as_uint(z0.x);
-            d[e + 1] = __float_as_uint(z0.y);
-            d[e + 2] = __float_as_uint(z1.x);
-            d[e + 3] = __float_as_uint(z1.y);
-          }
-          if (!whole) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (i + e < lo || i + e > hi) d[e] = 0;
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) p[e] = pack2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
-          st16(t_dp + mine + i / 2, p);
+        for (int e = 0; e < 32; e += 4) {
+          const float4 y = delta[e / 4];
+          const f2 z0 = mul2(pair_of(v + e), add2(pair_of(d + e), f2{y.x, y.y})),
+                   z1 = mul2(pair_of(v + e + 2), add2(pair_of(d + e + 2), f2{y.z, y.w}));
+          d[e] = __float_as_uint(z0.x);
+          d[e + 1] = __float_as_uint(z0.y);
+          d[e + 2] = __float_as_uint(z1.x);
+          d[e + 3] = __float_as_uint(z1.y);
         }
+        if (!whole) mask_zero(d, 0, lo, hi);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] = pack2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+        st16(t_dp + mine, p);
         st_wait();
         fence_before_sync();
         __syncwarp();
@@ -1358,47 +1429,45 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
       if (ok && cnt > 0) ok = all_sync(mbar_wait(&ctl.o_full, nu++ & 1, abort_flag));
       if (!ok) break;
       fence_after_sync();
+      constexpr int N = D / 4;
       const bool in = key < u.n;
       const size_t row = (size_t)u.row0 + (size_t)key * u.step;
-      bf16 *out_k = (bf16*)a.dk + row * a.lddk + (size_t)u.hk * D, *out_v = (bf16*)a.dv + row * a.lddv + (size_t)u.hk * D;
-      float* part = t.part_o + ((size_t)u.slot * 2 * kT + key) * D;
+      float* part = t.part_o + ((size_t)u.slot * 2 * kT + key) * D + N * quarter;
       float odd = 0.f;
 #pragma unroll
-      for (int j0 = 0; j0 < D; j0 += 32) {     // D / 2 columns of dk, then of dv
-        const int j = half * (D / 2) + j0 % (D / 2);
-        const bool is_k = j0 < D / 2;
-        uint32_t x[32];
-        float y[32];
+      for (int kv = 0; kv < 2; ++kv) {
+        uint32_t x[N];
+        float y[N];
         if (cnt > 0) {
-          ld32((is_k ? t_dk : t_dv) + lanes + j, x);
+          ldn<N>((kv ? t_dv : t_dk) + lanes + N * quarter, x);
           ld_wait();
         } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) x[e] = 0;
+          for (int e = 0; e < N; ++e) x[e] = 0;
         }
-        if (j0 + 32 == D && cnt > 0) {
+        if (kv && cnt > 0) {
           fence_before_sync();
           __syncwarp();
           if (lane == 0) mbar_arrive(&ctl.o_empty);
         }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
+        for (int e = 0; e < N; ++e) {
           odd = fmaf(__uint_as_float(x[e]), 0.f, odd);
-          y[e] = __uint_as_float(x[e]) * (is_k ? a.scale : 1.f);
+          y[e] = __uint_as_float(x[e]) * (kv ? 1.f : a.scale);
         }
         if (in) {
           if (u.parts == 1) {
-            store_bf16<32>((is_k ? out_k : out_v) + j, y);
+            store_bf16<N>((kv ? (bf16*)a.dv + row * a.lddv : (bf16*)a.dk + row * a.lddk) + (size_t)u.hk * D + N * quarter, y);
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(part + (is_k ? 0 : kT * D) + j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+            for (int e = 0; e < N; e += 4)
+              *reinterpret_cast<float4*>(part + kv * kT * D + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
           }
         }
       }
       unsigned bad = __ballot_sync(0xffffffffu, in && odd != 0.f);
       __syncwarp();
-      for (; bad; bad &= bad - 1) dkv_row<D>(s, a, t, u, 32 * q + __ffs(bad) - 1, half);
+      for (; bad; bad &= bad - 1) dkv_row<D>(s, a, t, u, 32 * q + __ffs(bad) - 1, quarter);
     }
     fence_before_sync();
   }
@@ -1495,11 +1564,11 @@ cudaError_t backward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const 
   const unsigned sms = device_sms();
   if (a.rows > 0) {
     const int groups = a.rows / s0.R;
-    // (more channels a lane mean fewer exchanges; registers hold as many rows as a group may have)
+    // (registers hold as many rows as a group may have)
     const auto blocks = [&](int C) { return dim3((unsigned)(((long long)groups * a.n_kv * (D / C) + 127) / 128)); };
     if (s0.R == 1) e = launch_after(k_gat_masks<D, 1, 8>, blocks(8), dim3(128), 0, st, true, s0, a, groups);
-    else if (s0.R <= 5) e = launch_after(k_gat_masks<D, 5, 8>, blocks(8), dim3(128), 0, st, true, s0, a, groups);
-    else if (s0.R <= 9) e = launch_after(k_gat_masks<D, 9, 4>, blocks(4), dim3(128), 0, st, true, s0, a, groups);
+    else if (s0.R <= 5) e = launch_after(k_gat_masks<D, 5, D / 32>, blocks(D / 32), dim3(128), 0, st, true, s0, a, groups);
+    else if (s0.R <= 9) e = launch_after(k_gat_masks<D, 9, D / 32>, blocks(D / 32), dim3(128), 0, st, true, s0, a, groups);
     else e = launch_after(k_gat_masks<D, 16, D / 32>, blocks(D / 32), dim3(128), 0, st, true, s0, a, groups);
     if (e != cudaSuccess) return e;
     Seqs s = sorted(s0, false);
