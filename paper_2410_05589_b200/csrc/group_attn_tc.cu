@@ -95,6 +95,12 @@ __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* r) {
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
       : "memory");
 }
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ex2(float x) {
@@ -340,29 +346,29 @@ __device__ __forceinline__ void alloc_tmem(uint32_t* where, int cols) {
 }
 
 // ---- forward ----------------------------------------------------------------------------------------
-// A persistent block an SM; a unit of its work are two neighbouring query tiles of a head, which share the key tiles
-// that pass through the ring.  Warp 0 issues the TMA loads, warp 1 the MMAs; eight warps per query tile, two threads a
-// row with half of the keys each, which tell each other their maxima (what bounds a step is the latency of its instructions: with
-// one thread a row a step took twice as long).  The queue of the tensor cores is O0 += P0 V, S0 of the next keys, O1 += P1 V, S1 of the next keys (P lies in
-// S's columns: they work in order), so that one tile's softmax runs beside the other's products.
+// Two blocks an SM, each with one query tile of a head: one's softmax runs beside the other's products.  Warp 0 issues
+// the TMA loads, warp 1 the MMAs, warps 2..5 own a row a thread.  S of the next key tile is issued behind O += P V of this
+// one (P lies in S's columns: the tensor cores work in order); K and V pass through a ring.
+// Measured against it (52 heads, 2 sequences, k = 8): one persistent block an SM with two query tiles that share the ring,
+// four warps a tile 510 us and eight 541, steps of 64 keys with two buffers of scores 681 (an MMA of 64 columns takes the
+// issuing thread as long as one of 128).
 template <int D>
 struct Fwd {
-  static constexpr int NS = D == 128 ? 5 : 10;   // of the ring
-  static constexpr int threads = 576;
-  static constexpr int row_bytes = 2048;       // what the two warps of a row tell each other
-  static constexpr int smem = (2 + NS) * kTileBytes<D> + row_bytes + 1024;
+  static constexpr int NS = D == 128 ? 2 : 4;   // slots of the ring
+  static constexpr int threads = 192, cols = 256;
+  static constexpr int smem = (1 + NS) * kTileBytes<D> + 2048;
 };
 struct FwdCtl {
-  uint64_t full[10], empty[10], q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_empty[2];
+  uint64_t full[4], empty[4], q_full, s_full, p_full, o_full;
   uint32_t tmem;
   int abort_flag;
 };
 
-// Half of the columns of row r of query tile x over its key tiles [i0, i1), by one warp and over the keys it sees alone.
+// Row r of the query tile over its key tiles [i0, i1), by one warp and over the keys it sees alone.
 template <int D>
-__device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const QueryWork<2> u, int x, int r, int half) {
+__device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const QueryWork<1> u, int r) {
   const int lane = threadIdx.x & 31, h = u.h;
-  const size_t row_q = (size_t)u.qrow(x) + r;
+  const size_t row_q = (size_t)u.qrow(0) + r;
   const TileRow tr(r, u.w.R);
   const bf16 *k = (const bf16*)a.k + (size_t)(h / a.per) * D, *v = (const bf16*)a.v + (size_t)(h / a.per) * D;
   float q[D / 32], o[D / 32], m = -INFINITY, l = 0.f;
@@ -371,8 +377,8 @@ __device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const Q
   for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
   for (int i = u.i0; i < u.i1; ++i) {
     int x0, n, lo, hi;
-    const int kind = u.w.tile(i, u.group(x), u.rows(x), x0, n);
-    tr.sees(kind, x0, n, u.group(x), u.rows(x), lo, hi);
+    const int kind = u.w.tile(i, u.group(0), u.rows(0), x0, n);
+    tr.sees(kind, x0, n, u.group(0), u.rows(0), lo, hi);
     for (int c = lo; c <= hi; ++c) {
       const size_t row = u.w.key_row(kind, x0 + c);
       float kx[D / 32], y[D / 32];
@@ -396,262 +402,188 @@ __device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const Q
   if (t.splits == 1) {
     bf16* dst = (bf16*)a.out + row_q * a.ldo + (size_t)h * D;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e)
-      if (e / (D / 64) == half) dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * inv);
-    if (lane == 0 && half == 0) a.lse[(size_t)h * a.rows + row_q] = lse;
+    for (int e = 0; e < D / 32; ++e) dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * inv);
+    if (lane == 0) a.lse[(size_t)h * a.rows + row_q] = lse;
   } else {
     const size_t at = ((size_t)u.split * a.n_heads + h) * a.rows + row_q;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e)
-      if (e / (D / 64) == half) t.part_o[at * D + lane + 32 * e] = o[e] * inv;
-    if (lane == 0 && half == 0) t.part_l[at] = lse;
+    for (int e = 0; e < D / 32; ++e) t.part_o[at * D + lane + 32 * e] = o[e] * inv;
+    if (lane == 0) t.part_l[at] = lse;
   }
 }
 
 template <int D>
-__global__ void __launch_bounds__(Fwd<D>::threads, 1)
+__global__ void __launch_bounds__(Fwd<D>::threads, 2)
 k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a,
           const __grid_constant__ TcArgs t) {
   using F = Fwd<D>;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  // (no room for a shift to the tiles' boundary: shared memory begins on it, or the call fails)
-  if (base != raw) {
-    if (threadIdx.x == 0) atomicOr(a.status, kStatTimeout);
-    return;
-  }
-  const uint32_t sq = base, ring = base + 2 * kTileBytes<D>;
-  unsigned char* s_row = smem_raw + (2 + F::NS) * kTileBytes<D>;
-  FwdCtl& ctl = *reinterpret_cast<FwdCtl*>(s_row + F::row_bytes);
+  const uint32_t sq = base, ring = base + kTileBytes<D>;
+  FwdCtl& ctl = *reinterpret_cast<FwdCtl*>(smem_raw + (base - raw) + (1 + F::NS) * kTileBytes<D>);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < F::NS; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&ctl.q_full[i], 1); mbar_init(&ctl.q_empty[i], 1);
-      mbar_init(&ctl.s_full[i], 1); mbar_init(&ctl.p_full[i], 8);
-      mbar_init(&ctl.o_full[i], 1); mbar_init(&ctl.o_empty[i], 8);
-    }
+    mbar_init(&ctl.q_full, 1);
+    mbar_init(&ctl.s_full, 1);
+    mbar_init(&ctl.p_full, 4);
+    mbar_init(&ctl.o_full, 1);
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
   }
   if (warp == 1) {
     __syncwarp();
-    alloc_tmem(&ctl.tmem, 512);
+    alloc_tmem(&ctl.tmem, F::cols);
     fence_before_sync();
   }
+  const QueryWork<1> u(s, a, t, blockIdx.x);
+  const int i0 = u.i0, i1 = u.i1, rows = u.rows(0), group = u.group(0), qrow = u.qrow(0);
   __syncthreads();
   fence_after_sync();
-  const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_o = tmem + 2 * kT;
+  const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_o = tmem + kT;
   volatile int* abort_flag = &ctl.abort_flag;
-  const int units = QueryWork<2>::count(s, a, t);
   pdl_wait();
 
   if (warp == 0) {
-    if (lane == 0) {
-      int it = 0, nq[2] = {0, 0};
+    if (lane == 0 && i0 < i1) {
+      load_rows<D>(sq, &maps.q, qrow, u.h * D, &ctl.q_full);
+      const int col = u.h / a.per * D;
+      int it = 0;
       bool ok = true;
-      auto slot_of = [&](uint32_t& dst, uint64_t*& bar) {   // the next slot of the ring, when it is free
-        const int slot = it % F::NS;
-        ok = mbar_wait(&ctl.empty[slot], ((it / F::NS) & 1) ^ 1, abort_flag);
-        dst = ring + slot * kTileBytes<D>;
-        bar = &ctl.full[slot];
-        ++it;
-        return ok;
-      };
-      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
-        if (unit >= units) continue;
-        const QueryWork<2> u(s, a, t, unit);
-        if (u.i0 == u.i1) continue;
-        for (int x = 0; ok && x < u.nt; ++x) {
-          ok = mbar_wait(&ctl.q_empty[x], (nq[x]++ & 1) ^ 1, abort_flag);
-          if (ok) load_rows<D>(sq + x * kTileBytes<D>, &maps.q, u.qrow(x), u.h * D, &ctl.q_full[x]);
-        }
-        const int col = u.h / a.per * D;
-        uint32_t dst;
-        uint64_t* bar;
-        for (int i = u.i0; ok && i < u.i1; ++i) {
-          for (int kv = 0; ok && kv < 2; ++kv)
-            for (int x = 0; ok && x < (i < u.w.n_shared ? 1 : u.nt); ++x) {
-              int x0, n;
-              const int kind = u.w.tile(i, u.group(x), u.rows(x), x0, n), row0 = kind == CTX ? u.w.kv0 : u.w.g0;
-              if (slot_of(dst, bar)) load_keys<D>(dst, kv ? &maps.v : &maps.k, kv ? &maps.vs : &maps.ks, kind, row0, s.R, x0, col, bar);
-            }
+      for (int i = i0; ok && i < i1; ++i) {
+        int x0, n;
+        const int kind = u.w.tile(i, group, rows, x0, n), row0 = kind == CTX ? u.w.kv0 : u.w.g0;
+        for (int kv = 0; ok && kv < 2; ++kv, ++it) {
+          const int slot = it % F::NS;
+          ok = mbar_wait(&ctl.empty[slot], ((it / F::NS) & 1) ^ 1, abort_flag);
+          if (ok) load_keys<D>(ring + slot * kTileBytes<D>, kv ? &maps.v : &maps.k, kv ? &maps.vs : &maps.ks, kind, row0, s.R, x0, col,
+                               &ctl.full[slot]);
         }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      int pos = 0, nq[2] = {0, 0}, np[2] = {0, 0};
-      bool ok = true;
-      auto wait_slot = [&](int it) {
-        ok = ok && mbar_wait(&ctl.full[it % F::NS], (it / F::NS) & 1, abort_flag);
-        fence_after_sync();
-        return ring + it % F::NS * kTileBytes<D>;
-      };
-      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
-        if (unit >= units) continue;
-        const QueryWork<2> u(s, a, t, unit);
-        if (u.i0 == u.i1) continue;
-        // S of query tile x with the key tile whose slots begin at `at`
-        auto scores = [&](int i, int at, int x) {
-          const bool own = i >= u.w.n_shared;
-          const uint32_t k = wait_slot(own ? at + x : at);
-          if (!ok) return;
-          mma_scores<D>(tmem + x * kT, desc_k(sq + x * kTileBytes<D>), desc_k(k));
-          mma_commit(&ctl.s_full[x]);
-          if (own || x == u.nt - 1) mma_commit(&ctl.empty[(own ? at + x : at) % F::NS]);
-          if (i == u.i1 - 1) mma_commit(&ctl.q_empty[x]);
-        };
-        for (int x = 0; ok && x < u.nt; ++x) {
-          ok = mbar_wait(&ctl.q_full[x], nq[x] & 1, abort_flag);
-          if (ok) scores(u.i0, pos, x);
-        }
-        for (int i = u.i0; ok && i < u.i1; ++i) {
-          const bool own = i >= u.w.n_shared;
-          const int next = pos + (own ? 2 * u.nt : 2);
-          for (int x = 0; ok && x < u.nt; ++x) {
-            const int vs = own ? pos + u.nt + x : pos + 1;
-            const uint32_t v = wait_slot(vs);
-            ok = ok && mbar_wait(&ctl.p_full[x], np[x]++ & 1, abort_flag);
-            if (ok && i == u.i0) ok = mbar_wait(&ctl.o_empty[x], (nq[x]++ & 1) ^ 1, abort_flag);
-            if (!ok) break;
-            fence_after_sync();
-            mma_sums<D, 64>(t_o + x * kT, tmem + x * kT, desc_mn(v), i > u.i0);
-            if (own || x == u.nt - 1) mma_commit(&ctl.empty[vs % F::NS]);
-            if (i == u.i1 - 1) mma_commit(&ctl.o_full[x]);
-            else scores(i + 1, next, x);
-          }
-          pos = next;
-        }
+    // (the whole warp walks, so that addresses and descriptors stay in uniform registers; one lane issues)
+    const bool leader = elect_one();
+    const int n = i1 - i0;
+    const uint64_t dq = desc_k(sq), dk = desc_k(ring), dv = desc_mn(ring);
+    bool ok = n > 0 && all_sync(mbar_wait(&ctl.q_full, 0, abort_flag));
+    auto scores = [&](int i) {
+      const int it = 2 * i, slot = it % F::NS;
+      ok = all_sync(mbar_wait(&ctl.full[slot], (it / F::NS) & 1, abort_flag));
+      if (!ok) return;
+      fence_after_sync();
+      if (leader) {
+        mma_scores<D>(tmem, dq, dk + slot * (kTileBytes<D> >> 4));
+        mma_commit(&ctl.s_full);
+        mma_commit(&ctl.empty[slot]);
       }
+      __syncwarp();
+    };
+    if (ok) scores(0);
+    for (int i = 0; ok && i < n; ++i) {
+      const int it = 2 * i + 1, slot = it % F::NS;
+      ok = all_sync(mbar_wait(&ctl.full[slot], (it / F::NS) & 1, abort_flag)) && all_sync(mbar_wait(&ctl.p_full, i & 1, abort_flag));
+      if (!ok) break;
+      fence_after_sync();
+      if (leader) {
+        mma_sums<D, kT>(t_o, tmem, dv + slot * (kTileBytes<D> >> 4), i > 0);
+        mma_commit(&ctl.empty[slot]);
+        if (i + 1 == n) mma_commit(&ctl.o_full);
+      }
+      __syncwarp();
+      if (i + 1 < n) scores(i + 1);
     }
   } else {
-    const int q = warp & 3, r = 32 * q + lane, x = (warp - 2) >> 3, half = ((warp - 2) >> 2) & 1;
-    const uint32_t lanes = (uint32_t)(32 * q) << 16, ts = tmem + x * kT + lanes + 64 * half, to = t_o + x * kT + lanes + half * (D / 2);
+    const int q = warp & 3, r = 32 * q + lane;
+    const uint32_t lanes = (uint32_t)(32 * q) << 16, ts = tmem + lanes, to = t_o + lanes;
     const float c = a.scale * kLog2e;
     const TileRow tr(r, s.R);
-    // what the two warps of a row tell each other: maxima (two steps' worth, bf16), at the end their sums
-    unsigned char* own = s_row + (4 * x + q) * 256;
-    unsigned short* tops = reinterpret_cast<unsigned short*>(own);
-    float* sums = reinterpret_cast<float*>(own);
-    auto meet = [&] { asm volatile("bar.sync %0, 64;" ::"r"(1 + 4 * x + q) : "memory"); };
-    int ns = 0, nu = 0;
-    // (a wait that gives up does not end the loop: the other warp of the row would wait for this one for good.  What is
-    // formed then is not used, and the waits that follow give up at once.)
-    for (int round = 0, unit; (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
-      if (unit >= units) continue;
-      const QueryWork<2> u(s, a, t, unit);
-      if (x >= u.nt) continue;
-      const int rows = u.rows(x), group = u.group(x);
-      float m = -INFINITY, l = 0.f;
-      for (int i = u.i0; i < u.i1; ++i, ++ns) {
-        mbar_wait(&ctl.s_full[x], ns & 1, abort_flag);
-        __syncwarp();
-        fence_after_sync();
-        uint32_t v[32];
-        ld32(ts, v);
-        int x0, n, lo, hi;
-        const int kind = u.w.tile(i, group, rows, x0, n);
-        tr.sees(kind, x0, n, group, rows, lo, hi);
-        lo -= 64 * half;
-        hi -= 64 * half;
-        const bool whole = all_sync(lo <= 0 && hi >= 63);
-        // (the scores are read twice: 64 of them leave no registers for anything else)
-        float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int i = i0; i < i1; ++i) {
+      int x0, n, lo, hi;
+      const int kind = u.w.tile(i, group, rows, x0, n);
+      tr.sees(kind, x0, n, group, rows, lo, hi);
+      const bool whole = all_sync(lo <= 0 && hi >= kT - 1);
+      ok = all_sync(mbar_wait(&ctl.s_full, (i - i0) & 1, abort_flag));
+      if (!ok) break;
+      fence_after_sync();
+      uint32_t v[kT];
 #pragma unroll
-        for (int j = 0; j < 64; j += 32) {
-          ld_wait();
-          const int see = whole ? kAll : chunk_sees(j, lo, hi);
-          if (see == kSome) mask_scores(v, j, lo, hi);
-          if (see != kNone) {
+      for (int j = 0; j < kT; j += 32) ld32(ts + j, v + j);
+      ld_wait();
+      if (!whole) {
 #pragma unroll
-            for (int k = 0; k < 32; k += 8)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) y[e] = max3(y[e], __uint_as_float(v[k + e]), __uint_as_float(v[k + 4 + e]));
-          }
-          ld32(ts + (j == 0 ? 32 : 0), v);   // (behind the second chunk: the first one again)
-        }
-        const unsigned short mine = __bfloat16_as_ushort(__float2bfloat16_ru(fmaxf(max3(y[0], y[1], y[2]), y[3])));
-        tops[(2 * (ns & 1) + half) * 32 + lane] = mine;
-        meet();
-        const float top = fmaxf(__uint_as_float((uint32_t)mine << 16), __uint_as_float((uint32_t)tops[(2 * (ns & 1) + 1 - half) * 32 + lane] << 16));
-        if (i == u.i0) {
-          m = top;
-        } else {
-          // the sums stay relative to an older maximum until one has grown by 2^kSlack (the products so far are
-          // complete: S of this tile was issued behind them)
-          const bool grown = (top - m) * c > kSlack;
-          if (__any_sync(0xffffffffu, grown)) {
-            const float f = grown ? ex2((m - top) * c) : 1.f;
-            l *= f;
-            if (grown) m = top;
-#pragma unroll 1
-            for (int j = 0; j < D / 2; j += 32) {
-              uint32_t o[32];
-              ld32(to + j, o);
-              ld_wait();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              st32(to + j, o);
-            }
-          }
-        }
-        const float ref = m > -INFINITY ? m * c : 0.f;
-        f2 sum = {0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 64; j += 32) {
-          uint32_t p[16];
-          ld_wait();
-          const int see = whole ? kAll : chunk_sees(j, lo, hi);
-          if (see == kNone) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) p[e] = 0;
-          } else {
-            if (see == kSome) mask_scores(v, j, lo, hi);
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const f2 z = fma2(pair_of(v + e), f2{c, c}, f2{-ref, -ref}), w = {ex2(z.x), ex2(z.y)};
-              sum = add2(sum, w);
-              p[e / 2] = pack2(w.x, w.y);
-            }
-          }
-          if (j == 0) ld32(ts + 32, v);
-          st16(ts + j / 2, p);
-        }
-        l += sum.x + sum.y;
-        st_wait();
-        fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl.p_full[x]);
+        for (int j = 0; j < kT; j += 32)
+          if (chunk_sees(j, lo, hi) != kAll) mask_scores(v + j, j, lo, hi);
       }
-      meet();
-      sums[32 * half + lane] = l;
-      meet();
-      l += sums[32 * (1 - half) + lane];
-      meet();
-      if (u.i0 < u.i1) mbar_wait(&ctl.o_full[x], nu++ & 1, abort_flag);
+      float y[4] = {m, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int j = 0; j < kT; j += 8)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = max3(y[e], __uint_as_float(v[j + e]), __uint_as_float(v[j + 4 + e]));
+      const float top = fmaxf(max3(y[0], y[1], y[2]), y[3]);
+      if (i == i0) {
+        m = top;
+      } else {
+        // the sums stay relative to an older maximum until one has grown by 2^kSlack (the products so far are
+        // complete: S of this tile was issued behind them)
+        const bool grown = (top - m) * c > kSlack;
+        if (__any_sync(0xffffffffu, grown)) {
+          const float f = grown ? ex2((m - top) * c) : 1.f;
+          l *= f;
+          if (grown) m = top;
+#pragma unroll 1
+          for (int j = 0; j < D; j += 16) {
+            uint32_t o[16];
+            ld16(to + j, o);
+            ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            st16(to + j, o);
+          }
+        }
+      }
+      const float ref = m > -INFINITY ? m * c : 0.f;
+      f2 sum0 = {0.f, 0.f}, sum1 = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < kT; j += 32) {
+        uint32_t p[16];
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          const f2 z0 = fma2(pair_of(v + j + e), f2{c, c}, f2{-ref, -ref}), z1 = fma2(pair_of(v + j + e + 2), f2{c, c}, f2{-ref, -ref});
+          const f2 w0 = {ex2(z0.x), ex2(z0.y)}, w1 = {ex2(z1.x), ex2(z1.y)};
+          sum0 = add2(sum0, w0);
+          sum1 = add2(sum1, w1);
+          p[e / 2] = pack2(w0.x, w0.y);
+          p[e / 2 + 1] = pack2(w1.x, w1.y);
+        }
+        st16(ts + j / 2, p);
+      }
+      l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+      st_wait();
+      fence_before_sync();
       __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.p_full);
+    }
+    if (ok && i0 < i1) ok = all_sync(mbar_wait(&ctl.o_full, 0, abort_flag));
+    if (ok) {
       fence_after_sync();
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const size_t row = (size_t)u.qrow(x) + r, at = ((size_t)u.split * a.n_heads + u.h) * a.rows + row;
-      bf16* dst = (bf16*)a.out + row * a.ldo + (size_t)u.h * D + half * (D / 2);
+      const size_t row = (size_t)qrow + r, at = ((size_t)u.split * a.n_heads + u.h) * a.rows + row;
+      bf16* dst = (bf16*)a.out + row * a.ldo + (size_t)u.h * D;
       float odd = l * 0.f;                   // no number once a sum is not finite
 #pragma unroll
-      for (int j = 0; j < D / 2; j += 32) {
+      for (int j = 0; j < D; j += 32) {
         uint32_t o[32];
         float y[32];
-        if (u.i0 < u.i1) {
+        if (i0 < i1) {
           ld32(to + j, o);
           ld_wait();
         } else {
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0;
-        }
-        if (j + 32 == D / 2 && u.i0 < u.i1) {    // read back: the next unit's products may overwrite it
-          fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&ctl.o_empty[x]);
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
@@ -664,22 +596,22 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
           } else {
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(t.part_o + at * D + half * (D / 2) + j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+              *reinterpret_cast<float4*>(t.part_o + at * D + j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
           }
         }
       }
-      if (r < rows && half == 0) {
+      if (r < rows) {
         const float lse = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
         if (t.splits == 1) a.lse[(size_t)u.h * a.rows + row] = lse;
         else t.part_l[at] = lse;
       }
       unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f);
       __syncwarp();
-      for (; bad; bad &= bad - 1) fwd_row<D>(a, t, u, x, 32 * q + __ffs(bad) - 1, half);
+      for (; bad; bad &= bad - 1) fwd_row<D>(a, t, u, 32 * q + __ffs(bad) - 1);
     }
     fence_before_sync();
   }
-  finish(tid, warp, abort_flag, a.status, tmem, 512);
+  finish(tid, warp, abort_flag, a.status, tmem, F::cols);
 }
 
 // Joins the parts of a row's keys: a warp per (row, head).
@@ -828,45 +760,55 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      int it = 0, nu = 0;   // tiles and units so far
-      bool ok = true;
-      // S and dP of tile number i (over all units)
-      auto issue = [&](int i, bool last) {
-        const int ks = i % F::NK, vs = i % F::NV;
-        ok = mbar_wait(&ctl.s_empty, (i & 1) ^ 1, abort_flag) && mbar_wait(&ctl.k_full[ks], (i / F::NK) & 1, abort_flag);
-        if (!ok) return;
-        fence_after_sync();
-        mma_scores<D>(tmem, desc_k(sq), desc_k(sk + ks * kTileBytes<D>));
+    const bool leader = elect_one();   // (see the forward kernel)
+    int it = 0, nu = 0;   // tiles and units so far
+    bool ok = true;
+    const uint64_t dq = desc_k(sq), dg = desc_k(so), dk = desc_k(sk), dv = desc_k(sv), dkm = desc_mn(sk);
+    constexpr int kStep = kTileBytes<D> >> 4;
+    // S and dP of tile number i (over all units)
+    auto issue = [&](int i, bool last) {
+      const int ks = i % F::NK, vs = i % F::NV;
+      ok = all_sync(mbar_wait(&ctl.s_empty, (i & 1) ^ 1, abort_flag)) && all_sync(mbar_wait(&ctl.k_full[ks], (i / F::NK) & 1, abort_flag));
+      if (!ok) return;
+      fence_after_sync();
+      if (leader) {
+        mma_scores<D>(tmem, dq, dk + ks * kStep);
         mma_commit(&ctl.s_full);
-        ok = mbar_wait(&ctl.v_full[vs], (i / F::NV) & 1, abort_flag);
-        if (!ok) return;
-        fence_after_sync();
-        mma_scores<D>(t_dp + (i & 1) * kT, desc_k(so), desc_k(sv + vs * kTileBytes<D>));
+      }
+      __syncwarp();
+      ok = all_sync(mbar_wait(&ctl.v_full[vs], (i / F::NV) & 1, abort_flag));
+      if (!ok) return;
+      fence_after_sync();
+      if (leader) {
+        mma_scores<D>(t_dp + (i & 1) * kT, dg, dv + vs * kStep);
         mma_commit(&ctl.dp_full[i & 1]);
         mma_commit(&ctl.v_empty[vs]);
         if (last) mma_commit(&ctl.q_empty);
-      };
-      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
-        if (unit >= units) continue;
-        const QueryWork<1> u(s, a, t, unit);
-        const int cnt = u.i1 - u.i0;
-        if (cnt == 0) continue;
-        ok = mbar_wait(&ctl.q_full, nu & 1, abort_flag);
-        if (ok) issue(it, cnt == 1);
-        for (int i = 0; ok && i < cnt; ++i, ++it) {
-          if (i + 1 < cnt) issue(it + 1, i + 2 == cnt);
-          ok = ok && mbar_wait(&ctl.ds_full, it & 1, abort_flag);
-          if (ok && i == 0) ok = mbar_wait(&ctl.o_empty, (nu & 1) ^ 1, abort_flag);
-          if (!ok) break;
-          fence_after_sync();
-          const int ks = it % F::NK;
-          mma_sums<D, 32>(t_o, t_dp + (it & 1) * kT, desc_mn(sk + ks * kTileBytes<D>), i > 0);
+      }
+      __syncwarp();
+    };
+    for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+      if (unit >= units) continue;
+      const QueryWork<1> u(s, a, t, unit);
+      const int cnt = u.i1 - u.i0;
+      if (cnt == 0) continue;
+      ok = all_sync(mbar_wait(&ctl.q_full, nu & 1, abort_flag));
+      if (ok) issue(it, cnt == 1);
+      for (int i = 0; ok && i < cnt; ++i, ++it) {
+        if (i + 1 < cnt) issue(it + 1, i + 2 == cnt);
+        ok = ok && all_sync(mbar_wait(&ctl.ds_full, it & 1, abort_flag));
+        if (ok && i == 0) ok = all_sync(mbar_wait(&ctl.o_empty, (nu & 1) ^ 1, abort_flag));
+        if (!ok) break;
+        fence_after_sync();
+        const int ks = it % F::NK;
+        if (leader) {
+          mma_sums<D, 32>(t_o, t_dp + (it & 1) * kT, dkm + ks * kStep, i > 0);
           mma_commit(&ctl.k_empty[ks]);
           if (i + 1 == cnt) mma_commit(&ctl.o_full);
         }
-        ++nu;
+        __syncwarp();
       }
+      ++nu;
     }
   } else {
     const int q = warp & 3, quarter = (warp - 2) >> 2, r = 32 * q + lane;
@@ -1289,50 +1231,63 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      int it = 0, nu = 0;
-      bool ok = true;
-      auto scores = [&](int i) {
-        ok = ok && mbar_wait(&ctl.q_full[i & 1], (i >> 1) & 1, abort_flag);
-        if (!ok) return;
-        fence_after_sync();
-        mma_scores<D>(tmem, desc_k(sk), desc_k(sq + (i & 1) * kTileBytes<D>));
+    const bool leader = elect_one();
+    int it = 0, nu = 0;
+    bool ok = true;
+    const uint64_t dk = desc_k(sk), dv = desc_k(sv), dq = desc_k(sq), dg = desc_k(sg), dqm = desc_mn(sq), dgm = desc_mn(sg);
+    constexpr int kStep = kTileBytes<D> >> 4;
+    auto scores = [&](int i) {
+      ok = ok && all_sync(mbar_wait(&ctl.q_full[i & 1], (i >> 1) & 1, abort_flag));
+      if (!ok) return;
+      fence_after_sync();
+      if (leader) {
+        mma_scores<D>(tmem, dk, dq + (i & 1) * kStep);
         mma_commit(&ctl.s_full);
-      };
-      auto dprob = [&](int i, bool last) {
-        ok = ok && mbar_wait(&ctl.g_full[i & 1], (i >> 1) & 1, abort_flag);
-        if (!ok) return;
-        fence_after_sync();
-        mma_scores<D>(t_dp, desc_k(sv), desc_k(sg + (i & 1) * kTileBytes<D>));
+      }
+      __syncwarp();
+    };
+    auto dprob = [&](int i, bool last) {
+      ok = ok && all_sync(mbar_wait(&ctl.g_full[i & 1], (i >> 1) & 1, abort_flag));
+      if (!ok) return;
+      fence_after_sync();
+      if (leader) {
+        mma_scores<D>(t_dp, dv, dg + (i & 1) * kStep);
         mma_commit(&ctl.dp_full);
         if (last) mma_commit(&ctl.k_empty);
-      };
-      for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
-        if (unit >= units) continue;
-        const KeyWork u(s, a, t, unit);
-        const int cnt = u.j1 - u.j0;
-        if (!u.there() || cnt == 0) continue;
-        ok = mbar_wait(&ctl.k_full, nu & 1, abort_flag);
-        scores(it);
-        dprob(it, cnt == 1);
-        for (int i = 0; ok && i < cnt; ++i, ++it) {
-          ok = mbar_wait(&ctl.p_full, it & 1, abort_flag);
-          if (ok && i == 0) ok = mbar_wait(&ctl.o_empty, (nu & 1) ^ 1, abort_flag);
-          if (!ok) break;
-          fence_after_sync();
-          mma_sums<D, 32>(t_dv, tmem, desc_mn(sg + (it & 1) * kTileBytes<D>), i > 0);
-          mma_commit(&ctl.g_empty[it & 1]);
-          if (i + 1 < cnt) scores(it + 1);
-          ok = ok && mbar_wait(&ctl.ds_full, it & 1, abort_flag);
-          if (!ok) break;
-          fence_after_sync();
-          mma_sums<D, 32>(t_dk, t_dp, desc_mn(sq + (it & 1) * kTileBytes<D>), i > 0);
-          mma_commit(&ctl.q_empty[it & 1]);
-          if (i + 1 < cnt) dprob(it + 1, i + 2 == cnt);
-          else mma_commit(&ctl.o_full);
-        }
-        ++nu;
       }
+      __syncwarp();
+    };
+    for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
+      if (unit >= units) continue;
+      const KeyWork u(s, a, t, unit);
+      const int cnt = u.j1 - u.j0;
+      if (!u.there() || cnt == 0) continue;
+      ok = all_sync(mbar_wait(&ctl.k_full, nu & 1, abort_flag));
+      scores(it);
+      dprob(it, cnt == 1);
+      for (int i = 0; ok && i < cnt; ++i, ++it) {
+        ok = all_sync(mbar_wait(&ctl.p_full, it & 1, abort_flag));
+        if (ok && i == 0) ok = all_sync(mbar_wait(&ctl.o_empty, (nu & 1) ^ 1, abort_flag));
+        if (!ok) break;
+        fence_after_sync();
+        if (leader) {
+          mma_sums<D, 32>(t_dv, tmem, dgm + (it & 1) * kStep, i > 0);
+          mma_commit(&ctl.g_empty[it & 1]);
+        }
+        __syncwarp();
+        if (i + 1 < cnt) scores(it + 1);
+        ok = ok && all_sync(mbar_wait(&ctl.ds_full, it & 1, abort_flag));
+        if (!ok) break;
+        fence_after_sync();
+        if (leader) {
+          mma_sums<D, 32>(t_dk, t_dp, dqm + (it & 1) * kStep, i > 0);
+          mma_commit(&ctl.q_empty[it & 1]);
+          if (i + 1 == cnt) mma_commit(&ctl.o_full);
+        }
+        __syncwarp();
+        if (i + 1 < cnt) dprob(it + 1, i + 2 == cnt);
+      }
+      ++nu;
     }
   } else if (warp == 2) {
     int it = 0;
@@ -1548,9 +1503,8 @@ cudaError_t forward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const T
   static std::atomic<uint64_t> done{0};
   if (cudaError_t e = ready(k_gat_fwd<D>, Fwd<D>::smem, done)) return e;
   Seqs s = sorted(s0, false);
-  const long long works = (long long)query_tiles(s, 2) * a.n_heads * t.splits;
-  cudaError_t e = launch_after(k_gat_fwd<D>, dim3((unsigned)std::min<long long>(works, device_sms())), dim3(Fwd<D>::threads),
-                               Fwd<D>::smem, st, true, maps, s, a, t);
+  const unsigned works = (unsigned)query_tiles(s, 1) * a.n_heads * t.splits;
+  cudaError_t e = launch_after(k_gat_fwd<D>, dim3(works), dim3(Fwd<D>::threads), Fwd<D>::smem, st, true, maps, s, a, t);
   if (e != cudaSuccess || t.splits == 1) return e;
   const long long units = (long long)a.rows * a.n_heads;
   return launch_after(k_gat_join<D>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, true, a, t);
@@ -1591,12 +1545,12 @@ cudaError_t backward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const 
 }  // namespace
 
 // Parts that a query tile's keys are dealt to, so that few query tiles still fill the device: as many as find room at
-// once (a block an SM), none with less than two key tiles.
+// once (two blocks an SM forward, one backward), none with less than two key tiles.
 int attn_splits(const Seqs& s, int n_heads, bool backward) {
   Seqs c = s;
-  const long long units = (long long)query_tiles(c, backward ? 1 : 2) * n_heads;
+  const long long units = (long long)query_tiles(c, 1) * n_heads, room = (backward ? 1 : 2) * device_sms();
   if (units == 0) return 1;
-  return std::max(1, (int)std::min<long long>(std::min<long long>(device_sms() / units, most_keys(s) / 2), 32));
+  return std::max(1, (int)std::min<long long>(std::min<long long>(room / units, most_keys(s) / 2), 32));
 }
 // Parts that a key tile's steps are dealt to, at most kParts: four units of work an SM, so that the last ones end at about
 // the same time although the first tiles of a sequence are seen by the most rows.
