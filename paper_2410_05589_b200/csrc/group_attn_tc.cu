@@ -81,13 +81,6 @@ template <int N>
 __device__ __forceinline__ void ldn(uint32_t taddr, uint32_t* r) {
   if constexpr (N == 32) ld32(taddr, r); else ld16(taddr, r);
 }
-__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::
-          "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
-      "r"(taddr)
-      : "memory");
-}
 __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(
@@ -927,9 +920,9 @@ __global__ void __launch_bounds__(256) k_gat_dq_join(const __grid_constant__ Att
 }
 
 // ---- backward: dk, dv of the masks, delta ------------------------------------------------------------------
-// A [MASK] row is seen by the R - j rows of its own group that follow it: too little for a matrix product.  The lanes of
-// a (group, key head) keep the group's keys, values and their gradients in registers, C neighbouring channels
-// each; they also form delta = dout . out of the rows they read anyway.  Bound by memory.
+// A [MASK] row is seen by the R - j rows of its own group that follow it: too little for a matrix product.  A warp per
+// (group, key head) keeps the group's keys, values and their gradients in registers, a lane D / 32 neighbouring
+// channels; it also forms delta = dout . out of the rows it reads anyway.  Bound by memory.
 template <int C>
 struct Chans { uint32_t v[C / 2]; };   // C neighbouring channels, bf16
 template <int C>
@@ -965,16 +958,38 @@ __device__ __forceinline__ float chan_dot(const Chans<C>& x, const Chans<C>& y) 
   return s;
 }
 
-// D / C lanes per (group, key head); RM: most rows of a group that the registers hold.
-template <int D, int RM, int C>
-__global__ void __launch_bounds__(128, RM <= 5 ? 4 : (RM <= 9 ? 3 : 2)) k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, int groups) {
-  constexpr int L = D / C;
+// Sums of N values (a power of two) over the warp: lane l ends with the sum of value l % N.  At each step a lane passes on the
+// half of its values that the other one keeps: N + 4 exchanges at most where one value at a time takes 5 N.
+template <int N>
+__device__ __forceinline__ float sum_many(float (&v)[N], int lane) {
+#pragma unroll
+  for (int n = N / 2; n > 0; n >>= 1) {
+    const bool up = lane & n;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float give = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, n);
+    }
+  }
+  float s = v[0];
+#pragma unroll
+  for (int o = N; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
+}
+
+// A warp per (group, key head), C channels a lane; RM: most rows of a group that the registers hold.  A row's scores and
+// dP of all masks it sees, and its delta, are summed over the lanes together; lane j - 1 then has mask j's.
+template <int D, int RM>
+__global__ void __launch_bounds__(128, RM <= 3 ? 4 : (RM <= 5 ? 3 : 2))
+k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, int groups) {
+  constexpr int C = D / 32, NM = RM - 1;                          // NM: masks
+  constexpr int N = NM <= 1 ? 4 : (NM <= 3 ? 8 : (NM <= 7 ? 16 : 32));   // scores, dP, delta
   pdl_launch_dependents();
   pdl_wait();
-  const int lane = threadIdx.x % L, R = s.R;
-  const long long unit = ((long long)blockIdx.x * 128 + threadIdx.x) / L;
-  const bool there = unit < (long long)groups * a.n_kv;   // (all lanes of a warp take part in its exchanges)
-  const int g = there ? (int)(unit / a.n_kv) : 0, hk = there ? (int)(unit - (long long)g * a.n_kv) : 0;
+  const int lane = threadIdx.x % 32, R = s.R;
+  const long long unit = (long long)blockIdx.x * 4 + threadIdx.x / 32;
+  if (unit >= (long long)groups * a.n_kv) return;
+  const int g = (int)(unit / a.n_kv), hk = (int)(unit - (long long)g * a.n_kv);
   int lo = 0, hi = s.B - 1;            // the sequence of group g: its rows begin at q0 / R
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -995,51 +1010,58 @@ __global__ void __launch_bounds__(128, RM <= 5 ? 4 : (RM <= 9 ? 3 : 2)) k_gat_ma
   const float c = a.scale * kLog2e;
   for (int h = hk * a.per; h < (hk + 1) * a.per; ++h) {
     float* delta_out = a.delta + (size_t)h * a.rows + q0;
-    const float* lse_in = a.lse + (size_t)h * a.rows + q0;
+    const float lse = lane < R ? a.lse[(size_t)h * a.rows + q0 + lane] * kLog2e : 0.f;   // lane i: of row i
     const bf16 *q_in = (const bf16*)a.q + q0 * a.ldq + (size_t)h * D + C * lane,
                *g_in = (const bf16*)a.dout + q0 * a.lddo + (size_t)h * D + C * lane,
                *o_in = (const bf16*)a.out + q0 * a.ldo + (size_t)h * D + C * lane;
-    // four rows' values in flight
-    constexpr int NB = RM < 5 ? RM : (RM == 5 ? 5 : 4);
+    constexpr int NB = RM <= 5 ? RM : 4;       // rows whose values are in flight
 #pragma unroll
     for (int i0 = 0; i0 < RM; i0 += NB) {
       if (i0 >= R) break;
       Chans<C> q[NB], d[NB], o[NB];
-      float lse[NB];
 #pragma unroll
       for (int x = 0; x < NB; ++x) {
         const int i = i0 + x;
         if (i < RM && i < R) {
           d[x] = chan_load<C>(g_in + i * a.lddo);
           o[x] = chan_load<C>(o_in + i * a.ldo);
-          if (i > 0) {
-            q[x] = chan_load<C>(q_in + i * a.ldq);
-            lse[x] = lse_in[i] * kLog2e;
-          }
+          if (i > 0) q[x] = chan_load<C>(q_in + i * a.ldq);
         }
       }
 #pragma unroll
       for (int x = 0; x < NB; ++x) {
         const int i = i0 + x;
         if (i >= RM || i >= R) break;
-        float delta = chan_dot(d[x], o[x]);
+        if (i == 0) {
+          float delta = chan_dot(d[x], o[x]);
 #pragma unroll
-        for (int w = L / 2; w > 0; w >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, w);
-        if (lane == 0 && there) delta_out[i] = delta;
+          for (int w = 16; w > 0; w >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, w);
+          if (lane == 0) delta_out[0] = delta;
+          continue;
+        }
+        float t[N];
+#pragma unroll
+        for (int y = 0; y < N; ++y) t[y] = 0.f;
 #pragma unroll
         for (int j = 1; j < RM; ++j) {
           if (j > i) break;
-          float sc = chan_dot(q[x], k[j]), dp = chan_dot(d[x], v[j]);
+          t[j - 1] = chan_dot(q[x], k[j]);
+          t[NM + j - 1] = chan_dot(d[x], v[j]);
+        }
+        t[2 * NM] = chan_dot(d[x], o[x]);
+        const float sum = sum_many<N>(t, lane);
+        const float delta = __shfl_sync(0xffffffffu, sum, 2 * NM), dp = __shfl_sync(0xffffffffu, sum, (lane + NM) & (N - 1)),
+                    ls = __shfl_sync(0xffffffffu, lse, i);
+        if (lane == 0) delta_out[i] = delta;
+        const float p = ex2(fmaf(sum, c, -ls)), ds = p * (dp - delta);    // lane j - 1: of mask j
 #pragma unroll
-          for (int w = L / 2; w > 0; w >>= 1) {
-            sc += __shfl_xor_sync(0xffffffffu, sc, w);
-            dp += __shfl_xor_sync(0xffffffffu, dp, w);
-          }
-          const float p = ex2(fmaf(sc, c, -lse[x])), ds = p * (dp - delta);
+        for (int j = 1; j < RM; ++j) {
+          if (j > i) break;
+          const float pj = __shfl_sync(0xffffffffu, p, j - 1), dsj = __shfl_sync(0xffffffffu, ds, j - 1);
 #pragma unroll
           for (int e = 0; e < C; ++e) {
-            dv[j][e] = fmaf(p, chan(d[x], e), dv[j][e]);
-            dk[j][e] = fmaf(ds, chan(q[x], e), dk[j][e]);
+            dv[j][e] = fmaf(pj, chan(d[x], e), dv[j][e]);
+            dk[j][e] = fmaf(dsj, chan(q[x], e), dk[j][e]);
           }
         }
       }
@@ -1047,7 +1069,7 @@ __global__ void __launch_bounds__(128, RM <= 5 ? 4 : (RM <= 9 ? 3 : 2)) k_gat_ma
   }
 #pragma unroll
   for (int j = 1; j < RM; ++j) {
-    if (j >= R || !there) break;
+    if (j >= R) break;
 #pragma unroll
     for (int e = 0; e < C; ++e) dk[j][e] *= a.scale;
     chan_store<C>((bf16*)a.dk + (k0 + j) * a.lddk + (size_t)hk * D + C * lane, dk[j]);
@@ -1519,11 +1541,12 @@ cudaError_t backward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const 
   if (a.rows > 0) {
     const int groups = a.rows / s0.R;
     // (registers hold as many rows as a group may have)
-    const auto blocks = [&](int C) { return dim3((unsigned)(((long long)groups * a.n_kv * (D / C) + 127) / 128)); };
-    if (s0.R == 1) e = launch_after(k_gat_masks<D, 1, 8>, blocks(8), dim3(128), 0, st, true, s0, a, groups);
-    else if (s0.R <= 5) e = launch_after(k_gat_masks<D, 5, D / 32>, blocks(D / 32), dim3(128), 0, st, true, s0, a, groups);
-    else if (s0.R <= 9) e = launch_after(k_gat_masks<D, 9, D / 32>, blocks(D / 32), dim3(128), 0, st, true, s0, a, groups);
-    else e = launch_after(k_gat_masks<D, 16, D / 32>, blocks(D / 32), dim3(128), 0, st, true, s0, a, groups);
+    const dim3 blocks((unsigned)(((long long)groups * a.n_kv + 3) / 4));
+    if (s0.R == 1) e = launch_after(k_gat_masks<D, 1>, blocks, dim3(128), 0, st, true, s0, a, groups);
+    else if (s0.R <= 3) e = launch_after(k_gat_masks<D, 3>, blocks, dim3(128), 0, st, true, s0, a, groups);
+    else if (s0.R <= 5) e = launch_after(k_gat_masks<D, 5>, blocks, dim3(128), 0, st, true, s0, a, groups);
+    else if (s0.R <= 9) e = launch_after(k_gat_masks<D, 9>, blocks, dim3(128), 0, st, true, s0, a, groups);
+    else e = launch_after(k_gat_masks<D, 16>, blocks, dim3(128), 0, st, true, s0, a, groups);
     if (e != cudaSuccess) return e;
     Seqs s = sorted(s0, false);
     const long long works = (long long)query_tiles(s, 1) * a.n_heads * tq.splits;
