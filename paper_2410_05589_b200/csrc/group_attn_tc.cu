@@ -1588,7 +1588,7 @@ void attn_parts(const Seqs& s, int n_kv, int per, TcArgs* t) {
 }
 
 bool attn_tc_takes(const AttnArgs& a, bool backward) {
-  auto fits = [](const void* p, size_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld < (1ull << 36); };
+  auto fits = [](const void* p, size_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld < (1ull << 34); };
   if (!(a.scale > 0.f)) return false;
   if (!fits(a.q, a.ldq) || !fits(a.k, a.ldk) || !fits(a.v, a.ldv) || !fits(a.out, a.ldo)) return false;
   return !backward || (fits(a.dout, a.lddo) && fits(a.dq, a.lddq) && fits(a.dk, a.lddk) && fits(a.dv, a.lddv));

@@ -20,45 +20,58 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 
 // ---- rows that count -----------------------------------------------------------------------------
-// One block numbers them (a running sum over 1024 rows at a time).
+// One block numbers them, 4096 rows at a time: a running sum of the threads' counts of four rows.
+constexpr int kPer = 4;
 __global__ void __launch_bounds__(1024) k_loss_rows(int rows, int rows_pad, int V, const int* __restrict__ labels, LossBuf b,
                                                     const float* __restrict__ lse_in, const float* __restrict__ dloss,
                                                     float* loss, float* lse) {
-  __shared__ int s_w[32];
+  __shared__ int s_w[2][32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_launch_dependents();
   pdl_wait();
   int base = 0;
-  for (int r0 = 0; r0 < rows; r0 += 1024) {
-    const int r = r0 + tid;
-    const int lab = r < rows ? labels[r] : -1;
-    const bool counts = lab >= 0 && lab < V;
-    const unsigned m = __ballot_sync(0xffffffffu, counts);
-    if (lane == 0) s_w[warp] = __popc(m);
-    __syncthreads();
-    int before = 0, all = 0;
-    for (int w = 0; w < 32; ++w) {
-      const int c = s_w[w];
-      if (w < warp) before += c;
-      all += c;
+  for (int r0 = 0, turn = 0; r0 < rows; r0 += 1024 * kPer, turn ^= 1) {
+    const int r = r0 + kPer * tid;
+    int lab[kPer], cnt = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) lab[e] = r + e < rows ? labels[r + e] : -1;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) cnt += lab[e] >= 0 && lab[e] < V;
+    int inc = cnt;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
     }
-    if (r < rows) {
-      const int i = counts ? base + before + __popc(m & ((1u << lane) - 1)) : -1;
-      b.slot[r] = i;
+    if (lane == 31) s_w[turn][warp] = inc;
+    __syncthreads();                     // (two buffers: the next turn's writers have passed this one's readers)
+    int of_warps = s_w[turn][lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, of_warps, o);
+      if (lane >= o) of_warps += y;
+    }
+    const int before = __shfl_sync(0xffffffffu, of_warps, warp > 0 ? warp - 1 : 0), all = __shfl_sync(0xffffffffu, of_warps, 31);
+    int i = base + (warp > 0 ? before : 0) + inc - cnt;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      if (r + e >= rows) break;
+      const bool counts = lab[e] >= 0 && lab[e] < V;
+      b.slot[r + e] = counts ? i : -1;
       if (counts) {
-        b.row_of[i] = r;
-        b.label[i] = lab;
+        b.row_of[i] = r + e;
+        b.label[i] = lab[e];
         if (lse_in) {
-          b.lse[i] = lse_in[r];
-          b.up[i] = dloss[r];
+          b.lse[i] = lse_in[r + e];
+          b.up[i] = dloss[r + e];
         }
+        ++i;
       } else if (loss) {
-        loss[r] = 0.f;
-        lse[r] = 0.f;
+        loss[r + e] = 0.f;
+        lse[r + e] = 0.f;
       }
     }
     base += all;
-    __syncthreads();
   }
   if (tid == 0) *b.n = base;
   for (int i = base + tid; i < rows_pad; i += 1024) {   // rows that only fill up a tile
@@ -116,21 +129,27 @@ __global__ void __launch_bounds__(256) k_loss_gather(int H, int tile, const T* _
   }
 }
 
-// Joins a row's tiles: a warp per compact row.
-__global__ void __launch_bounds__(256) k_loss_join(int rows_pad, int tiles, LossBuf b, float* loss, float* lse) {
+// Joins a row's tiles: a warp per compact row, four tiles a lane in flight.
+__global__ void __launch_bounds__(256) k_loss_join(int tiles, LossBuf b, float* loss, float* lse) {
   pdl_wait();
   const int i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (i >= *b.n) return;
+  const float2* part = b.part + (size_t)i * tiles;
   float m = -INFINITY, s = 0.f;
   bool nan = false;
-  for (int t = lane; t < tiles; t += 32) {
-    const float2 p = b.part[(size_t)t * rows_pad + i];
-    nan |= p.y != p.y;
-    if (p.x > m) {
-      s = s * exp2f((m - p.x) * kLog2e) + p.y;
-      m = p.x;
-    } else if (p.x > -INFINITY) {
-      s += p.y * exp2f((p.x - m) * kLog2e);
+  for (int t0 = lane; t0 < tiles; t0 += 128) {
+    float2 p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = t0 + 32 * e < tiles ? part[t0 + 32 * e] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      nan |= p[e].y != p[e].y;
+      if (p[e].x > m) {
+        s = s * exp2f((m - p[e].x) * kLog2e) + p[e].y;
+        m = p[e].x;
+      } else if (p[e].x > -INFINITY) {
+        s += p[e].y * exp2f((p[e].x - m) * kLog2e);
+      }
     }
   }
   float top = m;
@@ -150,9 +169,10 @@ __global__ void __launch_bounds__(256) k_loss_join(int rows_pad, int tiles, Loss
 
 // dx of a row from its sums; a block per row.
 template <class T>
-__global__ void __launch_bounds__(256) k_loss_dx(int H, int splits, size_t layer, LossBuf b, T* dx, size_t ldx, bool vec) {
+__global__ void __launch_bounds__(256) k_loss_dx(int H, int splits, int kb, int pairs, size_t layer, LossBuf b, T* dx, size_t ldx, bool vec) {
   pdl_wait();
   const int i = b.slot[blockIdx.x];
+  if (pairs > 0) splits = dx_splits(*b.n, H, kb, pairs);
   T* dst = dx + (size_t)blockIdx.x * ldx;
   const float* a = b.acc + (size_t)(i < 0 ? 0 : i) * H;
   for (int c = 4 * threadIdx.x; c < H; c += 1024) {
@@ -293,7 +313,7 @@ __global__ void __launch_bounds__(256) k_loss_logits(LossPlan p, LossBuf b, cons
         if (n0 + 4 * tx + j < nv && !(c[i][j] == -INFINITY)) s += exp2f((c[i][j] - top) * kLog2e);
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (in && tx == 0) b.part[(size_t)blockIdx.x * p.rows_pad + m] = make_float2(top, s);
+      if (in && tx == 0) b.part[(size_t)m * p.tiles + blockIdx.x] = make_float2(top, s);
     }
   }
 }
@@ -357,7 +377,7 @@ LossPlan make_plan(int dtype, int rows, int hidden, int vocab) {
   const int most = (int)std::max<size_t>(1024, kPieceBytes / per_row / 256 * 256);
   const int pieces = div_up(vocab, most);
   p.piece = div_up(div_up(vocab, pieces), 256) * 256;
-  p.splits = 1;
+  p.splits = p.tc ? kMaxSplits : 1;
   if (!p.tc) {   // enough blocks for dx: its tiles times the parts of a piece
     const int blocks = div_up(rows, kT) * div_up(hidden, kT);
     while (p.splits < 16 && blocks * p.splits < 2 * 148 && p.piece / (2 * p.splits) >= 64) p.splits *= 2;
@@ -463,7 +483,7 @@ extern "C" ps_status ps_lm_loss(int dtype, int rows, int hidden, int vocab, cons
       e = launch_after(k_loss_logits<false>, dim3(a.p.tiles, div_up(rows, kT)), dim3(256), 0, st, true, a.p, a.b, (const float*)w, 0, vocab);
   }
   if (e == cudaSuccess)
-    e = launch_after(k_loss_join, dim3(div_up(rows, 8)), dim3(256), 0, st, true, a.p.rows_pad, a.p.tiles, a.b, loss, lse);
+    e = launch_after(k_loss_join, dim3(div_up(rows, 8)), dim3(256), 0, st, true, a.p.tiles, a.b, loss, lse);
   return err.cuda(e, "ps_lm_loss");
 }
 
@@ -499,10 +519,10 @@ extern "C" ps_status ps_lm_loss_backward(int dtype, int rows, int hidden, int vo
     const size_t layer = (size_t)a.p.rows_pad * hidden;
     const bool vec = aligned(dx, 16) && lddx * es % 16 == 0;
     if (a.p.tc)
-      e = launch_after(k_loss_dx<__nv_bfloat16>, dim3(rows), dim3(256), 0, st, true, hidden, a.p.splits, layer, a.b,
-                       (__nv_bfloat16*)dx, lddx, vec);
+      e = launch_after(k_loss_dx<__nv_bfloat16>, dim3(rows), dim3(256), 0, st, true, hidden, a.p.splits, div_up(a.p.piece, 64),
+                       device_sms() / 2, layer, a.b, (__nv_bfloat16*)dx, lddx, vec);
     else
-      e = launch_after(k_loss_dx<float>, dim3(rows), dim3(256), 0, st, true, hidden, a.p.splits, layer, a.b, (float*)dx, lddx, vec);
+      e = launch_after(k_loss_dx<float>, dim3(rows), dim3(256), 0, st, true, hidden, a.p.splits, 0, 0, layer, a.b, (float*)dx, lddx, vec);
   }
   return err.cuda(e, "ps_lm_loss_backward");
 }

@@ -15,7 +15,7 @@ struct LossBuf {
   float *lse, *up;       // [rows_pad] of compact rows: lse and dloss (backward)
   void* x;               // [rows_pad][hidden] compact rows, dtype
   // forward: per vocabulary tile and compact row the maximum and the sum of exponentials against it
-  float2* part;          // [tiles][rows_pad]
+  float2* part;          // [rows_pad][tiles]
   float* picked;         // [rows_pad] logit of the label
   // backward
   void* g;               // [rows_pad][piece] gradient of a piece's logits
@@ -28,7 +28,7 @@ struct LossPlan {
   int rows, rows_pad, hidden, vocab;
   int tile_v, tiles;     // vocabulary rows of a tile of the forward pass
   int piece;             // vocabulary rows of a piece of the backward pass
-  int splits;            // parts of a piece that dx is summed over
+  int splits;            // parts of a piece that dx is summed over (tensor cores: at most, see dx_splits)
 };
 
 struct LossArgs {
@@ -39,6 +39,20 @@ struct LossArgs {
   bool want_dx;
   int* status;
 };
+
+// Parts of a piece's kb k blocks that the tensor cores' dx is dealt in: what a pair then works in sequence is least, in k blocks and
+// kTileCost of them for each tile's beginning and end.  (180 tiles on 74 pairs are three waves, of which two parts each make
+// five half ones: 13B, 2253 rows, 261 -> 216 us a piece.)
+constexpr int kMaxSplits = 4, kTileCost = 6, kLossTile = 256;
+__host__ __device__ inline int dx_splits(int rows, int hidden, int kb, int pairs) {
+  const int tiles = ((rows + kLossTile - 1) / kLossTile) * ((hidden + kLossTile - 1) / kLossTile);
+  int best = 1, least = 0;
+  for (int s = 1; s <= kMaxSplits; ++s) {
+    const int cost = (tiles * s + pairs - 1) / pairs * ((kb + s - 1) / s + kTileCost);
+    if (s == 1 || cost < least) { best = s; least = cost; }
+  }
+  return best;
+}
 
 // ---- lm_loss_tc.cu
 cudaError_t loss_forward_tc(const LossArgs& a, cudaStream_t st);

@@ -3,7 +3,7 @@
 //   forward   S = X W^T  -> per row and half tile: maximum, sum of exponentials
 //   gradient  S = X W^T  -> G = up (exp(S - lse) - onehot), rounded to bf16 (the operand type of the two products
 //                           that read it; what they add up is fp32)
-//   dx        G W        -> sums over the pieces in fp32
+//   dx        G W        -> sums over the pieces in fp32, a piece in up to four parts of its k (see dx_splits)
 //   dw        G^T X      -> the head's gradient
 //
 // Two CTAs (one cluster, the two SMs of a TPC) work on a tile of 256 x 256 with tcgen05.mma.cta_group::2: each
@@ -30,7 +30,7 @@ using umma::mbar_init;
 using umma::mbar_wait;
 using umma::smem_u32;
 
-constexpr int kTile = 256;                       // rows and columns of a pair's tile
+constexpr int kTile = kLossTile;                 // rows and columns of a pair's tile
 constexpr int kBK = 64;                          // k of a stage
 constexpr int kOpBytes = 128 * kBK * 2;          // one operand of one CTA
 constexpr int kStageBytes = 2 * kOpBytes;
@@ -57,6 +57,8 @@ struct Args {
   int m_tiles;         // DW: row tiles (vocabulary rows of the piece); else they follow from the rows that count
   int kb;              // k blocks; DW: they follow from the rows that count
   int v0, nv;
+  int kb_piece;        // DX: k blocks of a whole piece, which its parts are chosen by
+  int tiles;           // FWD: half tiles of a row
   bool add;            // DX: add to what is there
   __nv_bfloat16* dw;   // of the piece
   int* status;
@@ -159,7 +161,13 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
   const int n = *a.b.n;
   const int m_tiles = MODE == DW ? a.m_tiles : (n + kTile - 1) / kTile, n_tiles = (a.cols + kTile - 1) / kTile;
   const int kb = MODE == DW ? (n + kBK - 1) / kBK : a.kb;
-  const int tiles = m_tiles * n_tiles;
+  const int splits = MODE == DX ? dx_splits(n, a.hidden, a.kb_piece, n_pairs) : 1;
+  const int tiles = m_tiles * n_tiles * splits;
+  // Tile t: its place, and its part of the k blocks.
+  auto place = [&](int t, int& m, int& nn, int& part) {
+    part = MODE == DX ? t / (m_tiles * n_tiles) : 0;
+    tile_at(t - part * m_tiles * n_tiles, m_tiles, n_tiles, m, nn);
+  };
 
   if (warp == 0) {
     if (lane == 0) {   // ---- TMA producer
@@ -167,10 +175,10 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
       uint32_t parity = 1;
       bool alive = true;
       for (int t = pair; alive && t < tiles; t += n_pairs) {
-        int m, nn;
-        tile_at(t, m_tiles, n_tiles, m, nn);
+        int m, nn, part;
+        place(t, m, nn, part);
         const int ma = m * kTile + (int)rank * 128, nb = nn * kTile + (int)rank * 128;
-        for (int k = 0; k < kb; ++k) {
+        for (int k = kb * part / splits; k < kb * (part + 1) / splits; ++k) {
           if (!mbar_wait(&ctl.empty[st], parity, abort_flag)) { alive = false; break; }
           if (rank == 0) mbar_arrive_expect_tx(&ctl.full[st], 2 * kStageBytes);
           const uint32_t sa = base + st * kStageBytes, sb = sa + kOpBytes, bar = smem_u32(&ctl.full[st]) & kPeerMask;
@@ -202,14 +210,17 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
         if (!mbar_wait(&ctl.acc_empty[buf], ((c >> 1) & 1) ^ 1, abort_flag)) break;
         fence_after_sync();
         const uint32_t d = tmem + buf * kTile;
-        for (int k = 0; k < kb; ++k) {
+        int m, nn, part;
+        place(t, m, nn, part);
+        const int k0 = kb * part / splits, k1 = kb * (part + 1) / splits;
+        for (int k = k0; k < k1; ++k) {
           if (!mbar_wait(&ctl.full[st], parity, abort_flag)) { alive = false; break; }
           fence_after_sync();
           const uint32_t sa = base + st * kStageBytes;
           const uint64_t da = op_desc<A_MN>(sa), db = op_desc<B_MN>(sa + kOpBytes);
 #pragma unroll
           for (int s = 0; s < kBK / 16; ++s)
-            mma_pair(d, da + s * (A_MN ? 128 : 2), db + s * (B_MN ? 128 : 2), id, k > 0 || s > 0);
+            mma_pair(d, da + s * (A_MN ? 128 : 2), db + s * (B_MN ? 128 : 2), id, k > k0 || s > 0);
           commit_pair(&ctl.empty[st]);
           if (++st == kStages) { st = 0; parity ^= 1; }
         }
@@ -222,8 +233,8 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
     int c = 0;
     for (int t = pair; t < tiles; t += n_pairs, ++c) {
       const int buf = c & 1;
-      int mt, nt;
-      tile_at(t, m_tiles, n_tiles, mt, nt);
+      int mt, nt, part;
+      place(t, mt, nt, part);
       const bool ok = kb == 0 || mbar_wait(&ctl.acc_full[buf], (c >> 1) & 1, abort_flag);
       if (!__all_sync(0xffffffffu, ok)) break;
       fence_after_sync();
@@ -253,7 +264,7 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
           }
           sum += s0 + s1;
         }
-        if (m < n) a.b.part[(size_t)(2 * nt + half) * a.rows_pad + m] = make_float2(top, sum);
+        if (m < n) a.b.part[(size_t)m * a.tiles + 2 * nt + half] = make_float2(top, sum);
       } else if (MODE == GRAD) {
         const bool in = m < n;
         const float l = a.b.lse[m] * kLog2e, up = a.b.up[m];
@@ -275,11 +286,16 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
                                            pack2(v[j + 6], v[j + 7]));
         }
       } else if (MODE == DX) {
-        float* dst = a.b.acc + (size_t)m * a.hidden;
+        const bool none = kb * part / splits == kb * (part + 1) / splits;   // (fewer k blocks than parts)
+        float* dst = a.b.acc + ((size_t)part * a.rows_pad + m) * a.hidden;
 #pragma unroll 1
         for (int j0 = 0; j0 < 128; j0 += 32) {
           float v[32];
           tmem_ld32(ta + j0, v);
+          if (none) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = 0.f;
+          }
           if (m < n) {
 #pragma unroll
             for (int j = 0; j < 32; j += 4) {
@@ -363,6 +379,7 @@ cudaError_t loss_forward_tc(const LossArgs& a, cudaStream_t st) {
   Args g = common(a);
   g.cols = p.vocab;
   g.kb = (p.hidden + kBK - 1) / kBK;
+  g.tiles = p.tiles;
   return launch<FWD>(x, w, g, p.rows_pad / kTile * ((p.vocab + kTile - 1) / kTile), st);
 }
 
@@ -382,8 +399,9 @@ cudaError_t loss_piece_tc(const LossArgs& a, int v0, int nv, cudaStream_t st) {
     if (!make_map(&gk, a.b.g, p.rows_pad, p.piece, 128) || !make_map(&wm, w, nv, p.hidden, 64)) return cudaErrorNotSupported;
     g.cols = p.hidden;
     g.kb = (nv + kBK - 1) / kBK;
+    g.kb_piece = (p.piece + kBK - 1) / kBK;
     g.add = v0 > 0;
-    e = launch<DX>(gk, wm, g, mt * ht, st);
+    e = launch<DX>(gk, wm, g, device_sms() / 2, st);   // (the parts depend on the rows that count and on the number of pairs)
   }
   if (e == cudaSuccess && a.dw) {
     CUtensorMap gm, xm;
