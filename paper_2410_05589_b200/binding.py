@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 
 import torch
 
@@ -230,35 +231,57 @@ class _on:
             c.__exit__(*exc)
 
 
-def _need(ok, text):
-    if not ok:
-        raise PsError(-1, text)
+# (What these checks cost on the host is most of what a small call costs: texts are put together only for a refusal, a
+# tensor's device is read once.)
+def _refuse(text):
+    raise PsError(-1, text)
 
 
-def _tensors(first, *others, dtype=None):
+def _tensors(device, *tensors, dtype=None):
     """CUDA tensors of one device (None is skipped) and, with ``dtype``, of one type."""
-    _need(first.is_cuda, "tensors must lie on a CUDA device")
-    for t in (first, *others):
+    for t in tensors:
         if t is not None:
-            _need(t.device == first.device, "tensors lie on different devices")
-            _need(dtype is None or t.dtype == dtype, f"expected {dtype}, got {t.dtype}")
+            if t.device != device:
+                _refuse(f"tensors lie on different devices ({device}, {t.device})")
+            if dtype is not None and t.dtype != dtype:
+                _refuse(f"expected {dtype}, got {t.dtype}")
+
+
+def _first(t, name):
+    """Device and type code of the tensor that sets both."""
+    if not t.is_cuda:
+        _refuse("tensors must lie on a CUDA device")
+    code = _DTYPE_CODE.get(t.dtype)
+    if code is None:
+        _refuse(f"{name}: float32 or bfloat16, got {t.dtype}")
+    return t.device, code
 
 
 def _rows(t, width, name):
     """Row stride in elements of a tensor of rows that are dense; a view of a wider buffer may have a larger one."""
+    shape, stride = t.shape, t.stride()
     w = 1
-    for n, s in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        _need(n == 1 or s == w, f"{name}: rows must be dense")
-        w *= n
-    _need(w == width, f"{name}: rows of {w} values, expected {width}")
-    if t.shape[0] <= 1:
+    for i in range(len(shape) - 1, 0, -1):
+        if shape[i] != 1 and stride[i] != w:
+            _refuse(f"{name}: rows must be dense")
+        w *= shape[i]
+    if w != width:
+        _refuse(f"{name}: rows of {w} values, expected {width}")
+    if shape[0] <= 1:
         return width
-    _need(t.stride(0) >= width, f"{name}: rows overlap")
-    return t.stride(0)
+    if stride[0] < width:
+        _refuse(f"{name}: rows overlap")
+    return stride[0]
+
+
+_err = threading.local()
 
 
 def _op(fn, *args):
-    err = C.create_string_buffer(256)
+    try:
+        err = _err.text
+    except AttributeError:
+        err = _err.text = C.create_string_buffer(256)
     rc = fn(*args, err, 256, _stream())
     if rc != PS_OK:
         raise PsError(rc, err.value.decode())
@@ -269,30 +292,32 @@ def _ptr(t):
 
 
 def _scratch(nbytes, device):
-    _need(nbytes > 0, "sizes out of range")
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None   # (0: the call says why)
 
 
 def _group_args(q, k, v, n_ctx, n_groups, k_masks, scale):
-    _tensors(q, k, v, dtype=q.dtype)
-    _need(q.dtype in _DTYPE_CODE, f"q: float32 or bfloat16, got {q.dtype}")
-    _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.shape[2] == q.shape[2],
-          "q [rows][n_heads][head_dim], k and v [rows][n_kv_heads][head_dim]")
-    _need(len(n_ctx) == len(n_groups), "n_ctx and n_groups have one entry per sequence")
-    n_ctx, n_groups = [int(x) for x in n_ctx], [int(x) for x in n_groups]
+    device, code = _first(q, "q")
+    _tensors(device, k, v, dtype=q.dtype)
+    qs, ks = q.shape, k.shape
+    if len(qs) != 3 or len(ks) != 3 or ks != v.shape or ks[2] != qs[2]:
+        _refuse("q [rows][n_heads][head_dim], k and v [rows][n_kv_heads][head_dim]")
+    if len(n_ctx) != len(n_groups):
+        _refuse("n_ctx and n_groups have one entry per sequence")
     rows = sum(n_groups) * (k_masks + 1)
-    _need(q.shape[0] == rows and k.shape[0] == rows + sum(n_ctx), "the rows do not add up to the sequences")
-    d = q.shape[2]
-    a = ps_group_attn_args()
-    a.dtype, a.B, a.k_masks = _DTYPE_CODE[q.dtype], len(n_ctx), k_masks
-    a.n_heads, a.n_kv_heads, a.head_dim = q.shape[1], k.shape[1], d
-    a.n_ctx, a.n_groups = _iarr(n_ctx), _iarr(n_groups)
-    a.scale = d ** -0.5 if scale is None else float(scale)
-    wq, wk = q.shape[1] * d, k.shape[1] * d
-    a.q, a.k, a.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
-    a.ldq, a.ldk, a.ldv = _rows(q, wq, "q"), _rows(k, wk, "k"), _rows(v, wk, "v")
-    a.ldo, a.lddo, a.lddq, a.lddk, a.lddv = wq, wq, wq, wk, wk
-    return a
+    if qs[0] != rows or ks[0] != rows + sum(n_ctx):
+        _refuse("the rows do not add up to the sequences")
+    d = qs[2]
+    wq, wk = qs[1] * d, ks[1] * d
+    a = ps_group_attn_args(code, len(n_ctx), k_masks, qs[1], ks[1], d, _iarr(n_ctx), _iarr(n_groups),
+                           d ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                           _rows(q, wq, "q"), _rows(k, wk, "k"), _rows(v, wk, "v"), None, wq, None, None, wq, None, None, None,
+                           wq, wk, wk)
+    return a, device, wq, wk
+
+
+def _check_lse(lse, q):
+    if lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (q.shape[1], q.shape[0]):
+        _refuse("lse [n_heads][rows] float32")
 
 
 def group_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_ctx, n_groups, k_masks: int, scale=None,
@@ -303,21 +328,23 @@ def group_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_ctx, n_
     with a larger row stride allowed; n_ctx, n_groups: host lists, one entry per sequence; scale: head_dim ** -0.5 by
     default.  Returns ``out`` (like q) and ``lse`` [n_heads][group rows] float32; ``out`` may carry them preallocated.
     """
-    a = _group_args(q, k, v, n_ctx, n_groups, k_masks, scale)
+    a, device, wq, _ = _group_args(q, k, v, n_ctx, n_groups, k_masks, scale)
     lib = load_library()
-    with _on(q.device, stream):
+    with _on(device, stream):
         o = out if out is not None else {}
         if "out" not in o:
-            o["out"] = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            o["out"] = torch.empty(q.shape, dtype=q.dtype, device=device)
         if "lse" not in o:
-            o["lse"] = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-        _tensors(q, o["out"], dtype=q.dtype)
-        _tensors(q, o["lse"], status)
-        _need(o["out"].shape == q.shape and o["lse"].dtype == torch.float32 and o["lse"].is_contiguous() and
-              tuple(o["lse"].shape) == (q.shape[1], q.shape[0]), "out like q, lse [n_heads][rows] float32")
-        a.out, a.lse, a.ldo = o["out"].data_ptr(), o["lse"].data_ptr(), _rows(o["out"], q.shape[1] * q.shape[2], "out")
+            o["lse"] = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=device)
+        y, lse = o["out"], o["lse"]
+        _tensors(device, y, dtype=q.dtype)
+        _tensors(device, lse, status)
+        _check_lse(lse, q)
+        if y.shape != q.shape:
+            _refuse("out has another shape than q")
+        a.out, a.lse, a.ldo = y.data_ptr(), lse.data_ptr(), _rows(y, wq, "out")
         n = lib.ps_group_attn_workspace_bytes(C.byref(a), 0)
-        ws = _scratch(n, q.device) if n else None   # (0: the call says why)
+        ws = _scratch(n, device)
         _op(lib.ps_group_attn, C.byref(a), _ptr(ws), n, _ptr(status))
     return o
 
@@ -327,37 +354,47 @@ def group_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tenso
                              status=None, stream=None) -> dict:
     """ps_group_attn_backward: ``dq``, ``dk``, ``dv`` (like q, k, v) from dout, with out and lse of the forward call.
     ``grads`` may carry them preallocated, as views of wider buffers too."""
-    a = _group_args(q, k, v, n_ctx, n_groups, k_masks, scale)
+    a, device, wq, wk = _group_args(q, k, v, n_ctx, n_groups, k_masks, scale)
     lib = load_library()
-    wq, wk = q.shape[1] * q.shape[2], k.shape[1] * k.shape[2]
-    with _on(q.device, stream):
+    with _on(device, stream):
         o = grads if grads is not None else {}
         for name, like in (("dq", q), ("dk", k), ("dv", v)):
             if name not in o:
-                o[name] = torch.empty(like.shape, dtype=q.dtype, device=q.device)
-            _need(o[name].shape == like.shape, f"{name} has another shape than its tensor")
-        _tensors(q, dout, out, o["dq"], o["dk"], o["dv"], dtype=q.dtype)
-        _tensors(q, lse, status)
-        _need(dout.shape == q.shape and out.shape == q.shape, "dout and out like q")
-        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[1], q.shape[0]),
-              "lse [n_heads][rows] float32")
+                o[name] = torch.empty(like.shape, dtype=q.dtype, device=device)
+            elif o[name].shape != like.shape:
+                _refuse(f"{name} has another shape than its tensor")
+        dq, dk, dv = o["dq"], o["dk"], o["dv"]
+        _tensors(device, dout, out, dq, dk, dv, dtype=q.dtype)
+        _tensors(device, lse, status)
+        _check_lse(lse, q)
+        if dout.shape != q.shape or out.shape != q.shape:
+            _refuse("dout and out have the shape of q")
         a.out, a.lse, a.dout = out.data_ptr(), lse.data_ptr(), dout.data_ptr()
         a.ldo, a.lddo = _rows(out, wq, "out"), _rows(dout, wq, "dout")
-        a.dq, a.dk, a.dv = o["dq"].data_ptr(), o["dk"].data_ptr(), o["dv"].data_ptr()
-        a.lddq, a.lddk, a.lddv = _rows(o["dq"], wq, "dq"), _rows(o["dk"], wk, "dk"), _rows(o["dv"], wk, "dv")
+        a.dq, a.dk, a.dv = dq.data_ptr(), dk.data_ptr(), dv.data_ptr()
+        a.lddq, a.lddk, a.lddv = _rows(dq, wq, "dq"), _rows(dk, wk, "dk"), _rows(dv, wk, "dv")
         n = lib.ps_group_attn_workspace_bytes(C.byref(a), 1)
-        ws = _scratch(n, q.device) if n else None
+        ws = _scratch(n, device)
         _op(lib.ps_group_attn_backward, C.byref(a), _ptr(ws), n, _ptr(status))
     return o
 
 
 def _loss_args(x, w, labels):
-    _tensors(x, w, dtype=x.dtype)
-    _tensors(x, labels, dtype=None)
-    _need(x.dtype in _DTYPE_CODE, f"x: float32 or bfloat16, got {x.dtype}")
-    _need(x.dim() == 2 and w.dim() == 2 and w.shape[1] == x.shape[1] and w.is_contiguous(), "x [rows][hidden], w [vocab][hidden] dense")
-    _need(labels.dtype == torch.int32 and labels.is_contiguous() and tuple(labels.shape) == (x.shape[0],), "labels [rows] int32")
-    return _DTYPE_CODE[x.dtype], x.shape[0], x.shape[1], w.shape[0]
+    device, code = _first(x, "x")
+    _tensors(device, w, dtype=x.dtype)
+    _tensors(device, labels)
+    xs, wsh = x.shape, w.shape
+    if len(xs) != 2 or len(wsh) != 2 or wsh[1] != xs[1] or not w.is_contiguous():
+        _refuse("x [rows][hidden], w [vocab][hidden] dense")
+    if labels.dtype != torch.int32 or not labels.is_contiguous() or tuple(labels.shape) != (xs[0],):
+        _refuse("labels [rows] int32")
+    return device, (code, xs[0], xs[1], wsh[0])
+
+
+def _check_rows_of_floats(labels, **tensors):
+    for name, t in tensors.items():
+        if t.dtype != torch.float32 or not t.is_contiguous() or t.shape != labels.shape:
+            _refuse(f"{name} [rows] float32")
 
 
 def lm_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, out: dict | None = None, status=None,
@@ -367,19 +404,20 @@ def lm_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, out: dict | 
     x [rows][hidden] (a view with a larger row stride allowed), w [vocab][hidden], float32 or bfloat16; labels [rows]
     int32, any value outside the vocabulary (-100) for rows that count for nothing.  Returns ``loss`` and ``lse``
     [rows] float32, 0 for those rows."""
-    size = _loss_args(x, w, labels)
+    device, size = _loss_args(x, w, labels)
     lib = load_library()
-    with _on(x.device, stream):
+    with _on(device, stream):
         o = out if out is not None else {}
         for name in ("loss", "lse"):
             if name not in o:
-                o[name] = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-            _need(o[name].dtype == torch.float32 and o[name].is_contiguous() and o[name].shape == labels.shape, f"{name} [rows] float32")
-        _tensors(x, o["loss"], o["lse"], status)
+                o[name] = torch.empty(x.shape[0], dtype=torch.float32, device=device)
+        loss, lse = o["loss"], o["lse"]
+        _tensors(device, loss, lse, status)
+        _check_rows_of_floats(labels, loss=loss, lse=lse)
         n = lib.ps_lm_loss_workspace_bytes(*size, 0)
-        ws = _scratch(n, x.device) if n else None
-        _op(lib.ps_lm_loss, *size, _ptr(x), _rows(x, x.shape[1], "x"), _ptr(w), _ptr(labels), _ptr(o["loss"]), _ptr(o["lse"]),
-            _ptr(ws), n, _ptr(status))
+        ws = _scratch(n, device)
+        _op(lib.ps_lm_loss, *size, x.data_ptr(), _rows(x, x.shape[1], "x"), w.data_ptr(), labels.data_ptr(), loss.data_ptr(),
+            lse.data_ptr(), _ptr(ws), n, _ptr(status))
     return o
 
 
@@ -389,24 +427,25 @@ def lm_loss_backward(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, lse
     """ps_lm_loss_backward: ``dx`` (like x) and ``dw`` (like w) from dloss [rows] float32, the gradient of the caller's
     scalar with respect to each row's loss (1 / rows that count, for their mean), and lse of the forward call.
     ``grads`` may carry them preallocated."""
-    size = _loss_args(x, w, labels)
+    device, size = _loss_args(x, w, labels)
     lib = load_library()
-    with _on(x.device, stream):
+    with _on(device, stream):
         o = grads if grads is not None else {}
         for name, like, want in (("dx", x, want_dx), ("dw", w, want_dw)):
             if want and name not in o:
-                o[name] = torch.empty(like.shape, dtype=x.dtype, device=x.device)
+                o[name] = torch.empty(like.shape, dtype=x.dtype, device=device)
         dx, dw = o.get("dx") if want_dx else None, o.get("dw") if want_dw else None
-        _tensors(x, dx, dw, dtype=x.dtype)
-        _tensors(x, lse, dloss, status)
-        for t in (lse, dloss):
-            _need(t.dtype == torch.float32 and t.is_contiguous() and t.shape == labels.shape, "lse and dloss [rows] float32")
-        _need(dx is None or dx.shape == x.shape, "dx like x")
-        _need(dw is None or (dw.shape == w.shape and dw.is_contiguous()), "dw like w, dense")
+        _tensors(device, dx, dw, dtype=x.dtype)
+        _tensors(device, lse, dloss, status)
+        _check_rows_of_floats(labels, lse=lse, dloss=dloss)
+        if dx is not None and dx.shape != x.shape:
+            _refuse("dx has another shape than x")
+        if dw is not None and (dw.shape != w.shape or not dw.is_contiguous()):
+            _refuse("dw like w, dense")
         n = lib.ps_lm_loss_workspace_bytes(*size, 1)
-        ws = _scratch(n, x.device) if n else None
-        _op(lib.ps_lm_loss_backward, *size, _ptr(x), _rows(x, x.shape[1], "x"), _ptr(w), _ptr(labels), _ptr(lse), _ptr(dloss),
-            _ptr(dx), x.shape[1] if dx is None else _rows(dx, x.shape[1], "dx"), _ptr(dw), _ptr(ws), n, _ptr(status))
+        ws = _scratch(n, device)
+        _op(lib.ps_lm_loss_backward, *size, x.data_ptr(), _rows(x, x.shape[1], "x"), w.data_ptr(), labels.data_ptr(), lse.data_ptr(),
+            dloss.data_ptr(), _ptr(dx), x.shape[1] if dx is None else _rows(dx, x.shape[1], "dx"), _ptr(dw), _ptr(ws), n, _ptr(status))
     return o
 
 
@@ -415,20 +454,22 @@ def embed_rows(ids: torch.Tensor, table: torch.Tensor, mask_rows=None, scale: fl
     """ps_embed_rows: scaled rows of table [vocab][hidden] (ids below vocab) and of mask_rows [k_masks][hidden] (ids from
     vocab on); any other id gives a row of zeros.  ids [rows] int32; ``out`` [rows][hidden] may be a view with a
     larger row stride, such as the embedding half of the fc layer's input."""
-    _tensors(table, mask_rows, out, dtype=table.dtype)
-    _tensors(table, ids)
-    _need(table.dtype in _DTYPE_CODE, f"table: float32 or bfloat16, got {table.dtype}")
-    _need(table.dim() == 2 and table.is_contiguous() and ids.dim() == 1 and ids.dtype == torch.int32 and ids.is_contiguous(),
-          "table [vocab][hidden] dense, ids [rows] int32")
+    device, code = _first(table, "table")
+    _tensors(device, mask_rows, out, dtype=table.dtype)
+    _tensors(device, ids)
+    if table.dim() != 2 or not table.is_contiguous() or ids.dim() != 1 or ids.dtype != torch.int32 or not ids.is_contiguous():
+        _refuse("table [vocab][hidden] dense, ids [rows] int32")
     V, H = table.shape
-    _need(mask_rows is None or (mask_rows.dim() == 2 and mask_rows.shape[1] == H and mask_rows.is_contiguous()), "mask_rows [k_masks][hidden] dense")
+    if mask_rows is not None and (mask_rows.dim() != 2 or mask_rows.shape[1] != H or not mask_rows.is_contiguous()):
+        _refuse("mask_rows [k_masks][hidden] dense")
     lib = load_library()
-    with _on(table.device, stream):
+    with _on(device, stream):
         if out is None:
-            out = torch.empty((ids.shape[0], H), dtype=table.dtype, device=table.device)
-        _need(tuple(out.shape) == (ids.shape[0], H), "out [rows][hidden]")
-        _op(lib.ps_embed_rows, _DTYPE_CODE[table.dtype], ids.shape[0], H, V, 0 if mask_rows is None else mask_rows.shape[0],
-            _ptr(ids), _ptr(table), _ptr(mask_rows), float(scale), _ptr(out), _rows(out, H, "out"))
+            out = torch.empty((ids.shape[0], H), dtype=table.dtype, device=device)
+        elif tuple(out.shape) != (ids.shape[0], H):
+            _refuse("out [rows][hidden]")
+        _op(lib.ps_embed_rows, code, ids.shape[0], H, V, 0 if mask_rows is None else mask_rows.shape[0], ids.data_ptr(),
+            table.data_ptr(), _ptr(mask_rows), scale, out.data_ptr(), _rows(out, H, "out"))
     return out
 
 
@@ -436,26 +477,29 @@ def embed_rows_backward(ids: torch.Tensor, dout: torch.Tensor, vocab: int, k_mas
                         want_table: bool = True, want_mask: bool = True, grads: dict | None = None, stream=None) -> dict:
     """ps_embed_rows_backward: ``d_table`` [vocab][hidden] and ``d_mask`` [k_masks][hidden], the scaled sums of the rows of
     dout [rows][hidden] per id, zeros for ids without a row.  ``grads`` may carry them preallocated."""
-    _tensors(dout, ids)
-    _need(dout.dtype in _DTYPE_CODE, f"dout: float32 or bfloat16, got {dout.dtype}")
-    _need(dout.dim() == 2 and ids.dtype == torch.int32 and ids.is_contiguous() and tuple(ids.shape) == (dout.shape[0],),
-          "dout [rows][hidden], ids [rows] int32")
+    device, code = _first(dout, "dout")
+    _tensors(device, ids)
+    if dout.dim() != 2 or ids.dtype != torch.int32 or not ids.is_contiguous() or tuple(ids.shape) != (dout.shape[0],):
+        _refuse("dout [rows][hidden], ids [rows] int32")
     n_rows, H = dout.shape
     lib = load_library()
-    with _on(dout.device, stream):
+    with _on(device, stream):
         o = grads if grads is not None else {}
+        got = []
         for name, n, want in (("d_table", vocab, want_table), ("d_mask", k_masks, want_mask and k_masks > 0)):
+            t = None
             if want:
                 if name not in o:
-                    o[name] = torch.empty((n, H), dtype=dout.dtype, device=dout.device)
-                _tensors(dout, o[name], dtype=dout.dtype)
-                _need(tuple(o[name].shape) == (n, H) and o[name].is_contiguous(), f"{name} [{n}][hidden] dense")
-        dt, dm = o.get("d_table") if want_table else None, o.get("d_mask") if want_mask and k_masks > 0 else None
-        code = _DTYPE_CODE[dout.dtype]
+                    o[name] = torch.empty((n, H), dtype=dout.dtype, device=device)
+                t = o[name]
+                _tensors(device, t, dtype=dout.dtype)
+                if tuple(t.shape) != (n, H) or not t.is_contiguous():
+                    _refuse(f"{name} [{n}][hidden] dense")
+            got.append(t)
         n = lib.ps_embed_rows_workspace_bytes(code, n_rows, H, vocab, k_masks)
-        ws = _scratch(n, dout.device) if n else None
-        _op(lib.ps_embed_rows_backward, code, n_rows, H, vocab, k_masks, _ptr(ids), float(scale), _ptr(dout), _rows(dout, H, "dout"),
-            _ptr(dt), _ptr(dm), _ptr(ws), n)
+        ws = _scratch(n, device)
+        _op(lib.ps_embed_rows_backward, code, n_rows, H, vocab, k_masks, ids.data_ptr(), scale, dout.data_ptr(),
+            _rows(dout, H, "dout"), _ptr(got[0]), _ptr(got[1]), _ptr(ws), n)
     return o
 
 

@@ -33,9 +33,29 @@ __device__ __forceinline__ void st1(__nv_bfloat16* p, float x) { *p = __float2bf
 template <int D>
 constexpr int kPitch = D + 4;
 
-// Rows [0, n) of a tile to shared memory (zeros behind them); row i is src + (row0 + i step) ld.
+// Rows [0, n) of a tile to shared memory (zeros behind them); row i is src + (row0 + i step) ld.  Sixteen bytes a load where
+// pointer and stride allow it, all of a thread's loads in flight together.
 template <class T, int D>
 __device__ __forceinline__ void load_tile(float* s, const T* src, size_t ld, size_t row0, int step, int n) {
+  constexpr int N = 16 / sizeof(T), kLoads = kT * D / N / kThreads;
+  if ((((uintptr_t)src | (ld * sizeof(T))) & 15) == 0) {
+    uint4 x[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = threadIdx.x + i * kThreads, r = at / (D / N), c = at % (D / N) * N;
+      x[i] = make_uint4(0, 0, 0, 0);
+      if (r < n) x[i] = *reinterpret_cast<const uint4*>(src + (row0 + (size_t)r * step) * ld + c);
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = threadIdx.x + i * kThreads, r = at / (D / N), c = at % (D / N) * N;
+      const T* e = reinterpret_cast<const T*>(&x[i]);
+#pragma unroll
+      for (int j = 0; j < N; j += 4)
+        *reinterpret_cast<float4*>(s + r * kPitch<D> + c + j) = make_float4(ld1(e + j), ld1(e + j + 1), ld1(e + j + 2), ld1(e + j + 3));
+    }
+    return;
+  }
   for (int i = threadIdx.x; i < kT * D; i += kThreads) {
     const int r = i / D, c = i % D;
     s[r * kPitch<D> + c] = r < n ? ld1(src + (row0 + (size_t)r * step) * ld + c) : 0.f;
