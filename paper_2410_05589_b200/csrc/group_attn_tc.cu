@@ -647,7 +647,7 @@ struct Dq {
   static constexpr int smem = (2 + NK + NV) * kTileBytes<D> + 2048;
 };
 struct DqCtl {
-  uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2], q_full, q_empty, s_full, s_empty, dp_full[2], ds_full, o_full, o_empty;
+  uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2], q_full, q_empty, s_empty, dp_full[2], ds_full, o_full, o_empty;   // (dp_full: S and dP)
   uint32_t tmem;
   int abort_flag;
 };
@@ -704,7 +704,6 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
     for (int i = 0; i < F::NV; ++i) { mbar_init(&ctl.v_full[i], 1); mbar_init(&ctl.v_empty[i], 1); }
     mbar_init(&ctl.q_full, 2);
     mbar_init(&ctl.q_empty, 1);
-    mbar_init(&ctl.s_full, 1);
     mbar_init(&ctl.s_empty, 16);
     mbar_init(&ctl.dp_full[0], 1);
     mbar_init(&ctl.dp_full[1], 1);
@@ -764,10 +763,7 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
       ok = all_sync(mbar_wait(&ctl.s_empty, (i & 1) ^ 1, abort_flag)) && all_sync(mbar_wait(&ctl.k_full[ks], (i / F::NK) & 1, abort_flag));
       if (!ok) return;
       fence_after_sync();
-      if (leader) {
-        mma_scores<D>(tmem, dq, dk + ks * kStep);
-        mma_commit(&ctl.s_full);
-      }
+      if (leader) mma_scores<D>(tmem, dq, dk + ks * kStep);
       __syncwarp();
       ok = all_sync(mbar_wait(&ctl.v_full[vs], (i / F::NV) & 1, abort_flag));
       if (!ok) return;
@@ -817,11 +813,13 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
       const size_t row = (size_t)u.qrow(0) + r, at = (size_t)u.h * a.rows + row;
       const float lse = r < rows ? a.lse[at] * kLog2e : 0.f, delta = r < rows ? a.delta[at] : 0.f;
       for (int i = u.i0; i < u.i1; ++i, ++it) {
-        ok = all_sync(mbar_wait(&ctl.s_full, it & 1, abort_flag));
+        const uint32_t td = t_dp + (it & 1) * kT + mine;
+        ok = all_sync(mbar_wait(&ctl.dp_full[it & 1], (it >> 1) & 1, abort_flag));
         if (!ok) break;
         fence_after_sync();
         uint32_t v[32], d[32], p[16];
         ld32(tmem + mine, v);
+        ld32(td, d);
         int x0, n, lo, hi;
         const int kind = u.w.tile(i, u.group(0), rows, x0, n);
         tr.sees(kind, x0, n, u.group(0), rows, lo, hi);
@@ -838,12 +836,6 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
           v[j] = __float_as_uint(ex2(z.x));
           v[j + 1] = __float_as_uint(ex2(z.y));
         }
-        const uint32_t td = t_dp + (it & 1) * kT + mine;
-        ok = all_sync(mbar_wait(&ctl.dp_full[it & 1], (it >> 1) & 1, abort_flag));
-        if (!ok) break;
-        fence_after_sync();
-        ld32(td, d);
-        ld_wait();
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
           const f2 z = mul2(pair_of(v + e), add2(pair_of(d + e), f2{-delta, -delta}));
