@@ -16,6 +16,10 @@
 //   k_embed_join   adds the partial sums of an id that crosses blocks, in order.
 // [MASK] ids name a row of every group (thousands of rows each): pieces of 32 keep them from being one
 // block's work.
+// Measured (with the launches' gaps): 10235 rows of 4096 bf16 forward 26 us (3.9 TB/s; most rows are [MASK] rows that come from
+// L2, so that it is the writes); forward and the whole gradient of a table of 128256 x 4096, 10140 rows, 233 us (5.3
+// TB/s), of which the zeros take 173 (6.0 TB/s); the [MASK] gradients alone, 2547 rows of 5120, with the forward 31 us,
+// which is four launches' latency.  Sixteen rows of a block in flight instead of eight made the table's gradient 249 us.
 #include "train_ops.cuh"
 
 namespace ps {

@@ -196,10 +196,10 @@ __device__ __forceinline__ void mask_zero(uint32_t* w, int j, int lo, int hi) {
 }
 
 // ---- tiles ------------------------------------------------------------------------------------------
-// Key tiles that one or two query tiles of a sequence go through, in order: the context, the real rows up to those
-// of the last group, then (R > 1) each query tile's own rows.
+// Key tiles that a query tile of a sequence goes through, in order: the context, the real rows up to those of its last
+// group, then (R > 1) its own rows.
 struct KeyWalk {
-  int ctx, R, n_real;              // n_real: groups up to the last of the query tiles
+  int ctx, R, n_real;              // n_real: groups up to the last of the query tile
   int n_ctx, n_shared, total;
   int kv0, g0;                     // first context row, first group row of the sequence
   __device__ void start(const Seqs& s, int b, int group_end) {
@@ -210,8 +210,8 @@ struct KeyWalk {
     n_shared = n_ctx + div_up(n_real, kT);
     total = n_shared + (R > 1);
   }
-  // Kind of tile i, its first key's index among those of its kind and their number; for the query tile whose first
-  // group is `group` and that has n_rows.
+  // Kind of tile i, its first key's index among those of its kind and their number; the query tile begins with group
+  // `group` and has n_rows.
   __device__ int tile(int i, int group, int n_rows, int& x0, int& n) const {
     if (i < n_ctx) { x0 = i * kT; n = min(kT, ctx - x0); return CTX; }
     if (i < n_shared) { x0 = (i - n_ctx) * kT; n = min(kT, n_real - x0); return REAL; }
@@ -233,12 +233,11 @@ struct TileRow {
   }
 };
 
-// One unit of work of the kernels whose lanes are query rows: up to NT neighbouring query tiles of a head and a
-// part of their key tiles.  (It goes by value, and its two tiles' fields by selection, to stay in registers: as an object in
-// memory it was read again behind every instruction that may touch memory.)
-template <int NT>
+// One unit of work of the kernels whose lanes are query rows: a query tile of a head and a part of its key tiles.  (It
+// goes by value, to stay in registers: as an object in memory it was read again behind every instruction that may touch
+// memory.)
 struct QueryWork {
-  int b, h, split, nt, group0, group1, rows0, rows1, qrow0, i0, i1, gpt;
+  int b, h, split, group, rows, qrow, i0, i1;   // first group, rows, first row of the tile; key tiles [i0, i1)
   KeyWalk w;
   __device__ static int count(const Seqs& s, const AttnArgs& a, const TcArgs& t) { return s.tile0[s.B] * a.n_heads * t.splits; }
   // (unit 0 is the last one: the longest rows of the longest sequence)
@@ -247,17 +246,13 @@ struct QueryWork {
     split = 0;
     if (t.splits > 1) { split = u % t.splits; u /= t.splits; }
     const int tile = u / a.n_heads;
-    gpt = t.gpt;
     h = u - tile * a.n_heads;
     b = seq_of_tile(s, tile);
-    group0 = (tile - s.tile0[b]) * NT * gpt;
-    group1 = group0 + gpt;
-    const int left = s.groups[b] - group0;
-    rows0 = min(gpt, left) * s.R;
-    rows1 = NT == 1 ? 0 : max(0, min(gpt, left - gpt)) * s.R;
-    nt = rows1 > 0 ? 2 : 1;
-    qrow0 = s.q0[b] + group0 * s.R;
-    w.start(s, b, group0 + min(NT * gpt, left));
+    group = (tile - s.tile0[b]) * t.gpt;
+    const int n = min(t.gpt, s.groups[b] - group);
+    rows = n * s.R;
+    qrow = s.q0[b] + group * s.R;
+    w.start(s, b, group + n);
     i0 = 0;
     i1 = w.total;
     if (t.splits > 1) {
@@ -265,10 +260,6 @@ struct QueryWork {
       i1 = w.total * (split + 1) / t.splits;
     }
   }
-  // Of query tile x: first group, rows, first row.
-  __device__ int group(int x) const { return x ? group1 : group0; }
-  __device__ int rows(int x) const { return x ? rows1 : rows0; }
-  __device__ int qrow(int x) const { return qrow0 + x * gpt * w.R; }
 };
 
 // 128 rows of K or V (columns col ..) to shared memory.
@@ -342,9 +333,11 @@ __device__ __forceinline__ void alloc_tmem(uint32_t* where, int cols) {
 // Two blocks an SM, each with one query tile of a head: one's softmax runs beside the other's products.  Warp 0 issues
 // the TMA loads, warp 1 the MMAs, warps 2..5 own a row a thread.  S of the next key tile is issued behind O += P V of this
 // one (P lies in S's columns: the tensor cores work in order); K and V pass through a ring.
-// Measured against it (52 heads, 2 sequences, k = 8): one persistent block an SM with two query tiles that share the ring,
-// four warps a tile 510 us and eight 541, steps of 64 keys with two buffers of scores 681 (an MMA of 64 columns takes the
-// issuing thread as long as one of 128).
+// Measured (52 heads, 2 sequences, k = 8): 450 us.  One persistent block an SM with two query tiles that share the ring: four
+// warps a tile 510, eight 541, steps of 64 keys with two buffers of scores 639 (an MMA of 64 columns takes as long as one of
+// 128).  A quarter of the exponentials as polynomials on the FMA units: 485.
+// What bounds it: of 2000 cycles a step and tile the MMAs are 1024 and the exponentials (16 a cycle) as many; the rest is the
+// latency of the two hand-overs between the warps and the tensor cores, which two blocks hide by half.
 template <int D>
 struct Fwd {
   static constexpr int NS = D == 128 ? 2 : 4;   // slots of the ring
@@ -359,9 +352,9 @@ struct FwdCtl {
 
 // Row r of the query tile over its key tiles [i0, i1), by one warp and over the keys it sees alone.
 template <int D>
-__device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const QueryWork<1> u, int r) {
+__device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const QueryWork u, int r) {
   const int lane = threadIdx.x & 31, h = u.h;
-  const size_t row_q = (size_t)u.qrow(0) + r;
+  const size_t row_q = (size_t)u.qrow + r;
   const TileRow tr(r, u.w.R);
   const bf16 *k = (const bf16*)a.k + (size_t)(h / a.per) * D, *v = (const bf16*)a.v + (size_t)(h / a.per) * D;
   float q[D / 32], o[D / 32], m = -INFINITY, l = 0.f;
@@ -370,8 +363,8 @@ __device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const Q
   for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
   for (int i = u.i0; i < u.i1; ++i) {
     int x0, n, lo, hi;
-    const int kind = u.w.tile(i, u.group(0), u.rows(0), x0, n);
-    tr.sees(kind, x0, n, u.group(0), u.rows(0), lo, hi);
+    const int kind = u.w.tile(i, u.group, u.rows, x0, n);
+    tr.sees(kind, x0, n, u.group, u.rows, lo, hi);
     for (int c = lo; c <= hi; ++c) {
       const size_t row = u.w.key_row(kind, x0 + c);
       float kx[D / 32], y[D / 32];
@@ -430,8 +423,8 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
     alloc_tmem(&ctl.tmem, F::cols);
     fence_before_sync();
   }
-  const QueryWork<1> u(s, a, t, blockIdx.x);
-  const int i0 = u.i0, i1 = u.i1, rows = u.rows(0), group = u.group(0), qrow = u.qrow(0);
+  const QueryWork u(s, a, t, blockIdx.x);
+  const int i0 = u.i0, i1 = u.i1, rows = u.rows, group = u.group, qrow = u.qrow;
   __syncthreads();
   fence_after_sync();
   const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_o = tmem + kT;
@@ -641,6 +634,9 @@ __global__ void __launch_bounds__(256) k_gat_join(const __grid_constant__ AttnAr
 // the keys each.  The scores pass through registers, so that the next tile's are formed as soon as they are read; dP has
 // two buffers, and dS takes dP's columns (each quarter its own): the tensor cores work on S, dP of the next tile and dQ of the
 // last one while the warps turn this one's into dS.
+// Measured: 13B heads, 4 sequences of 150-420 groups of 5 rows, 177 us; 2047 groups on 8 key heads 305.  Steps of 64 keys in three
+// buffers, two groups of warps taking turns: 217 and 427.  What bounds it: 3300 cycles a step of which the MMAs are 1536
+// and the exponentials 1024; the rest is the latency of the loads from tensor memory, stores to it and barriers.
 template <int D>
 struct Dq {
   static constexpr int NK = 3, NV = 2, threads = 576;
@@ -654,9 +650,9 @@ struct DqCtl {
 
 // A quarter of the columns of row r of the query tile, by one warp and over the keys the row sees alone.
 template <int D>
-__device__ __noinline__ void dq_row(const AttnArgs& a, const TcArgs& t, const QueryWork<1> u, int r, int quarter) {
+__device__ __noinline__ void dq_row(const AttnArgs& a, const TcArgs& t, const QueryWork u, int r, int quarter) {
   const int lane = threadIdx.x & 31, h = u.h;
-  const size_t row_q = (size_t)u.qrow(0) + r;
+  const size_t row_q = (size_t)u.qrow + r;
   const TileRow tr(r, u.w.R);
   const bf16 *k = (const bf16*)a.k + (size_t)(h / a.per) * D, *v = (const bf16*)a.v + (size_t)(h / a.per) * D;
   float q[D / 32], g[D / 32], o[D / 32];
@@ -667,8 +663,8 @@ __device__ __noinline__ void dq_row(const AttnArgs& a, const TcArgs& t, const Qu
   for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
   for (int i = u.i0; i < u.i1; ++i) {
     int x0, n, lo, hi;
-    const int kind = u.w.tile(i, u.group(0), u.rows(0), x0, n);
-    tr.sees(kind, x0, n, u.group(0), u.rows(0), lo, hi);
+    const int kind = u.w.tile(i, u.group, u.rows, x0, n);
+    tr.sees(kind, x0, n, u.group, u.rows, lo, hi);
     for (int c = lo; c <= hi; ++c) {
       const size_t row = u.w.key_row(kind, x0 + c);
       float x[D / 32], y[D / 32];
@@ -723,7 +719,7 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
   fence_after_sync();
   const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_dp = tmem + kT, t_o = tmem + 3 * kT;
   volatile int* abort_flag = &ctl.abort_flag;
-  const int units = QueryWork<1>::count(s, a, t);
+  const int units = QueryWork::count(s, a, t);
   pdl_wait();
 
   if (warp == 0) {
@@ -732,16 +728,16 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
       bool ok = true;
       for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
         if (unit >= units) continue;
-        const QueryWork<1> u(s, a, t, unit);
+        const QueryWork u(s, a, t, unit);
         if (u.i0 == u.i1) continue;
         ok = mbar_wait(&ctl.q_empty, (nu++ & 1) ^ 1, abort_flag);
         if (!ok) break;
-        load_rows<D>(sq, &maps.q, u.qrow(0), u.h * D, &ctl.q_full);
-        load_rows<D>(so, &maps.dout, u.qrow(0), u.h * D, &ctl.q_full);
+        load_rows<D>(sq, &maps.q, u.qrow, u.h * D, &ctl.q_full);
+        load_rows<D>(so, &maps.dout, u.qrow, u.h * D, &ctl.q_full);
         const int col = u.h / a.per * D;
         for (int i = u.i0; i < u.i1; ++i, ++it) {
           int x0, n;
-          const int kind = u.w.tile(i, u.group(0), u.rows(0), x0, n), row0 = kind == CTX ? u.w.kv0 : u.w.g0, ks = it % F::NK, vs = it % F::NV;
+          const int kind = u.w.tile(i, u.group, u.rows, x0, n), row0 = kind == CTX ? u.w.kv0 : u.w.g0, ks = it % F::NK, vs = it % F::NV;
           ok = mbar_wait(&ctl.k_empty[ks], ((it / F::NK) & 1) ^ 1, abort_flag);
           if (!ok) break;
           load_keys<D>(sk + ks * kTileBytes<D>, &maps.k, &maps.ks, kind, row0, s.R, x0, col, &ctl.k_full[ks]);
@@ -778,7 +774,7 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
     };
     for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
       if (unit >= units) continue;
-      const QueryWork<1> u(s, a, t, unit);
+      const QueryWork u(s, a, t, unit);
       const int cnt = u.i1 - u.i0;
       if (cnt == 0) continue;
       ok = all_sync(mbar_wait(&ctl.q_full, nu & 1, abort_flag));
@@ -808,9 +804,9 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
     bool ok = true;
     for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
       if (unit >= units) continue;
-      const QueryWork<1> u(s, a, t, unit);
-      const int rows = u.rows(0), cnt = u.i1 - u.i0;
-      const size_t row = (size_t)u.qrow(0) + r, at = (size_t)u.h * a.rows + row;
+      const QueryWork u(s, a, t, unit);
+      const int rows = u.rows, cnt = u.i1 - u.i0;
+      const size_t row = (size_t)u.qrow + r, at = (size_t)u.h * a.rows + row;
       const float lse = r < rows ? a.lse[at] * kLog2e : 0.f, delta = r < rows ? a.delta[at] : 0.f;
       for (int i = u.i0; i < u.i1; ++i, ++it) {
         const uint32_t td = t_dp + (it & 1) * kT + mine;
@@ -821,8 +817,8 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
         ld32(tmem + mine, v);
         ld32(td, d);
         int x0, n, lo, hi;
-        const int kind = u.w.tile(i, u.group(0), rows, x0, n);
-        tr.sees(kind, x0, n, u.group(0), rows, lo, hi);
+        const int kind = u.w.tile(i, u.group, rows, x0, n);
+        tr.sees(kind, x0, n, u.group, rows, lo, hi);
         lo -= 32 * quarter;
         hi -= 32 * quarter;
         const bool whole = all_sync(lo <= 0 && hi >= 31);
@@ -914,7 +910,9 @@ __global__ void __launch_bounds__(256) k_gat_dq_join(const __grid_constant__ Att
 // ---- backward: dk, dv of the masks, delta ------------------------------------------------------------------
 // A [MASK] row is seen by the R - j rows of its own group that follow it: too little for a matrix product.  A warp per
 // (group, key head) keeps the group's keys, values and their gradients in registers, a lane D / 32 neighbouring
-// channels; it also forms delta = dout . out of the rows it reads anyway.  Bound by memory.
+// channels; it also forms delta = dout . out of the rows it reads anyway.
+// Measured: 6650 rows of 40 heads 110 us (409 MB, 3.7 TB/s); 10235 rows of 32 heads on 8, 89 us.  Bound by the latency of a
+// warp's loads: its registers leave room for 12 warps an SM (with spills at 16 and 20 it took 129 and 136 us).
 template <int C>
 struct Chans { uint32_t v[C / 2]; };   // C neighbouring channels, bf16
 template <int C>
@@ -1075,6 +1073,10 @@ k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, 
 // in its columns), dK and dV.  The warps form P^T while the tensor cores work on dK and dP^T, and dS^T while they work on
 // dV and the next step's S^T.  A thread owns a key and a quarter of the query columns, whose lse and delta a
 // warp of its own puts into shared memory.
+// Measured: 13B heads, 4 sequences of 150-420 groups of 5 rows, 185 us; 2047 groups on 8 key heads 326, in one part per key tile
+// 576 (the first tiles are seen by all 10235 rows of four heads, the last ones by few).  Steps of 64 rows with two groups of
+// warps taking turns: 224 and 405.  What bounds it: 4500 cycles a step, of which the MMAs are 2048; tensor memory has no room
+// for a second step's scores of 128 rows, so that the two halves of a step wait for each other's products.
 template <int D>
 struct Dkv {
   static constexpr int threads = 608;
@@ -1469,10 +1471,10 @@ __global__ void __launch_bounds__(256) k_gat_dkv_join(const __grid_constant__ Se
 }
 
 // ---- host ------------------------------------------------------------------------------------------------
-// Units of query tiles, nt at a time.
-int query_tiles(Seqs& s, int nt) {
+// Tiles of the sequences, numbered; returns how many.
+int query_tiles(Seqs& s) {
   s.tile0[0] = 0;
-  for (int b = 0; b < s.B; ++b) s.tile0[b + 1] = s.tile0[b] + div_up(s.groups[b], nt * groups_per_tile(kT, s.R));
+  for (int b = 0; b < s.B; ++b) s.tile0[b + 1] = s.tile0[b] + div_up(s.groups[b], groups_per_tile(kT, s.R));
   return s.tile0[s.B];
 }
 int key_tiles(Seqs& s) {
@@ -1517,7 +1519,7 @@ cudaError_t forward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const T
   static std::atomic<uint64_t> done{0};
   if (cudaError_t e = ready(k_gat_fwd<D>, Fwd<D>::smem, done)) return e;
   Seqs s = sorted(s0, false);
-  const unsigned works = (unsigned)query_tiles(s, 1) * a.n_heads * t.splits;
+  const unsigned works = (unsigned)query_tiles(s) * a.n_heads * t.splits;
   cudaError_t e = launch_after(k_gat_fwd<D>, dim3(works), dim3(Fwd<D>::threads), Fwd<D>::smem, st, true, maps, s, a, t);
   if (e != cudaSuccess || t.splits == 1) return e;
   const long long units = (long long)a.rows * a.n_heads;
@@ -1541,7 +1543,7 @@ cudaError_t backward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const 
     else e = launch_after(k_gat_masks<D, 16>, blocks, dim3(128), 0, st, true, s0, a, groups);
     if (e != cudaSuccess) return e;
     Seqs s = sorted(s0, false);
-    const long long works = (long long)query_tiles(s, 1) * a.n_heads * tq.splits;
+    const long long works = (long long)query_tiles(s) * a.n_heads * tq.splits;
     e = launch_after(k_gat_dq<D>, dim3((unsigned)std::min<long long>(works, sms)), dim3(Dq<D>::threads), Dq<D>::smem, st, true, maps,
                      s, a, tq);
     if (e == cudaSuccess && tq.splits > 1) {
@@ -1563,7 +1565,7 @@ cudaError_t backward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const 
 // once (two blocks an SM forward, one backward), none with less than two key tiles.
 int attn_splits(const Seqs& s, int n_heads, bool backward) {
   Seqs c = s;
-  const long long units = (long long)query_tiles(c, 1) * n_heads, room = (backward ? 1 : 2) * device_sms();
+  const long long units = (long long)query_tiles(c) * n_heads, room = (backward ? 1 : 2) * device_sms();
   if (units == 0) return 1;
   return std::max(1, (int)std::min<long long>(std::min<long long>(room / units, most_keys(s) / 2), 32));
 }

@@ -14,7 +14,11 @@
 //
 // Persistent pairs walk the tiles, eight row tiles of a column side by side, so that the pairs that work at one
 // time share both operands in L2.  Two accumulators in tensor memory let a tile's epilogue overlap the
-// next tile's products.  Warp 0 issues the TMA loads, warp 1 the MMAs (of the pair: in the leader CTA), warps
+// next tile's products.
+// What bounds it: the tensor cores, at the clock that the power limit leaves them.  Launches by themselves (cool device):
+// logits of 3890 rows, 4096 x 128256, 1.60 PFLOP/s, their gradient 1.63, dW 1.75, dx (sums read and written per piece) 1.44; a
+// whole call, forward and backward, 1.23 PFLOP/s of all four products against 1.40 that a library's product alone
+// sustains.  Up to 256 rows one tile of rows takes the vocabulary at 6.2 TB/s.  Warp 0 issues the TMA loads, warp 1 the MMAs (of the pair: in the leader CTA), warps
 // 2..9 read the sums back.  Every wait is bounded: on expiry the kernel raises the status word and returns.
 #include "lm_loss.cuh"
 #include "umma_gemm.cuh"
