@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kThreads) k_ga_fwd(const __grid_constant__ Seq
 
 // delta = dout . out, a warp per (row, head).
 template <class T, int D>
-__global__ void __launch_bounds__(256) k_ga_delta(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(256) k_ga_delta(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a) {
   pdl_launch_dependents();
   pdl_wait();
   const long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -252,6 +252,19 @@ __global__ void __launch_bounds__(256) k_ga_delta(const __grid_constant__ AttnAr
   const int r = (int)(u / a.n_heads), h = (int)(u - (long long)r * a.n_heads);
   const T *x = (const T*)a.dout + (size_t)r * a.lddo + (size_t)h * D, *y = (const T*)a.out + (size_t)r * a.ldo + (size_t)h * D;
   float d = 0.f;
+  if (sizeof(T) == 2) {
+    int lo = 0, hi = s.B - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s.q0[mid] <= r) lo = mid; else hi = mid - 1;
+    }
+    const int rho = r - s.q0[lo], n = s.ctx[lo] + rho / s.R + 1 + rho % s.R;
+    if (n <= kExactKeys) {
+      d = delta_of_keys<T, D>(s, a, lo, rho, h, n);
+      if (lane == 0) a.delta[(size_t)h * a.rows + r] = d;
+      return;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) d = fmaf(ld1(x + lane + 32 * i), ld1(y + lane + 32 * i), d);
 #pragma unroll
@@ -416,10 +429,10 @@ cudaError_t forward(Seqs s, const AttnArgs& a, cudaStream_t st) {
   return launch_after(k_ga_fwd<T, D>, dim3(tiles, a.n_heads), dim3(kThreads), smem, st, true, s, a);
 }
 template <class T, int D>
-cudaError_t delta_rows(const AttnArgs& a, cudaStream_t st) {
+cudaError_t delta_rows(const Seqs& s, const AttnArgs& a, cudaStream_t st) {
   if (a.rows == 0) return cudaSuccess;
   const long long units = (long long)a.rows * a.n_heads;
-  return launch_after(k_ga_delta<T, D>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, true, a);
+  return launch_after(k_ga_delta<T, D>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, true, s, a);
 }
 template <class T, int D>
 cudaError_t backward(Seqs s, const AttnArgs& a, cudaStream_t st) {
@@ -429,7 +442,7 @@ cudaError_t backward(Seqs s, const AttnArgs& a, cudaStream_t st) {
   if (cudaError_t e = allow_smem((const void*)k_ga_dkv<T, D>, smem_kv, done_kv)) return e;
   cudaError_t e = cudaSuccess;
   if (a.rows > 0) {
-    e = delta_rows<T, D>(a, st);
+    e = delta_rows<T, D>(s, a, st);
     if (e != cudaSuccess) return e;
     const int tiles = number_tiles(s, [&](int, int g) { return div_up(g, groups_per_tile(kT, s.R)); });
     e = launch_after(k_ga_dq<T, D>, dim3(tiles, a.n_heads), dim3(kThreads), smem_q, st, true, s, a);

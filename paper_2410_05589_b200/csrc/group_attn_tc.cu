@@ -948,6 +948,21 @@ __device__ __forceinline__ float chan_dot(const Chans<C>& x, const Chans<C>& y) 
   return s;
 }
 
+// delta of the rows with few keys (see kExactKeys): the first groups of sequences with a short context.  A warp per (row, head).
+__host__ __device__ inline int few_groups(int ctx, int groups) { return ctx >= kExactKeys ? 0 : (groups < kExactKeys - ctx ? groups : kExactKeys - ctx); }
+template <int D>
+__global__ void __launch_bounds__(256) k_gat_few(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int u = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (u >= s.tile0[s.B] * a.n_heads) return;            // tile0: such rows before the sequence
+  const int i = u / a.n_heads, h = u - i * a.n_heads, b = seq_of_tile(s, i), rho = i - s.tile0[b];
+  const int n = s.ctx[b] + rho / s.R + 1 + rho % s.R;
+  if (n > kExactKeys) return;
+  const float d = delta_of_keys<bf16, D>(s, a, b, rho, h, n);
+  if (lane == 0) a.delta[(size_t)h * a.rows + s.q0[b] + rho] = d;
+}
+
 // Sums of N values (a power of two) over the warp: lane l ends with the sum of value l % N.  At each step a lane passes on the
 // half of its values that the other one keeps: N + 4 exchanges at most where one value at a time takes 5 N.
 template <int N>
@@ -986,6 +1001,7 @@ k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, 
     if (s.q0[mid] <= g * R) lo = mid; else hi = mid - 1;
   }
   const size_t q0 = (size_t)g * R, k0 = (size_t)s.kv0[lo] + s.ctx[lo] + (q0 - s.q0[lo]);
+  const int n0 = s.ctx[lo] + g - s.q0[lo] / R + 1;   // keys that the group's first row sees
   Chans<C> k[RM], v[RM];
   float dk[RM][C], dv[RM][C];
 #pragma unroll
@@ -1026,7 +1042,7 @@ k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, 
           float delta = chan_dot(d[x], o[x]);
 #pragma unroll
           for (int w = 16; w > 0; w >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, w);
-          if (lane == 0) delta_out[0] = delta;
+          if (lane == 0 && n0 > kExactKeys) delta_out[0] = delta;
           continue;
         }
         float t[N];
@@ -1040,9 +1056,12 @@ k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, 
         }
         t[2 * NM] = chan_dot(d[x], o[x]);
         const float sum = sum_many<N>(t, lane);
-        const float delta = __shfl_sync(0xffffffffu, sum, 2 * NM), dp = __shfl_sync(0xffffffffu, sum, (lane + NM) & (N - 1)),
+        float delta = __shfl_sync(0xffffffffu, sum, 2 * NM);
+        const bool few = n0 + i <= kExactKeys;        // (k_gat_few has it)
+        if (few) delta = delta_out[i];
+        const float dp = __shfl_sync(0xffffffffu, sum, (lane + NM) & (N - 1)),
                     ls = __shfl_sync(0xffffffffu, lse, i);
-        if (lane == 0) delta_out[i] = delta;
+        if (lane == 0 && !few) delta_out[i] = delta;
         const float p = ex2(fmaf(sum, c, -ls)), ds = p * (dp - delta);    // lane j - 1: of mask j
 #pragma unroll
         for (int j = 1; j < RM; ++j) {
@@ -1534,6 +1553,13 @@ cudaError_t backward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const 
   const unsigned sms = device_sms();
   if (a.rows > 0) {
     const int groups = a.rows / s0.R;
+    Seqs f = s0;
+    f.tile0[0] = 0;
+    for (int b = 0; b < f.B; ++b) f.tile0[b + 1] = f.tile0[b] + few_groups(f.ctx[b], f.groups[b]) * f.R;
+    if (const int few = f.tile0[f.B]) {
+      e = launch_after(k_gat_few<D>, dim3(div_up(few * a.n_heads, 8)), dim3(256), 0, st, true, f, a);
+      if (e != cudaSuccess) return e;
+    }
     // (registers hold as many rows as a group may have)
     const dim3 blocks((unsigned)(((long long)groups * a.n_kv + 3) / 4));
     if (s0.R == 1) e = launch_after(k_gat_masks<D, 1>, blocks, dim3(128), 0, st, true, s0, a, groups);

@@ -113,3 +113,28 @@ def test_embedding_rows_and_their_gradients(ps, shape, dtype):
     got |= ps.embed_rows_backward(ids, dout, V, k, scale=1.7)
     val, bnd = ref.embed(ids, table, masks, 1.7, dout)
     ref.check(got, val, bnd, ("out", "d_table", "d_mask") if k else ("out", "d_table"))
+
+
+@pytest.mark.parametrize("odd", [False, True], ids=["aligned", "odd"])
+@pytest.mark.parametrize("shape", [([0], [1], 1, 4, 1), ([1], [1], 0, 8, 8), ([0], [3], 4, 6, 2), ([0, 60], [2, 2], 3, 4, 4)],
+                         ids=lambda s: f"c{sum(s[0])}g{sum(s[1])}k{s[2]}")
+def test_gradients_of_rows_with_few_keys(ps, shape, odd):
+    """p (dP - delta) is a difference of near numbers where one of a few keys has most of the weight: a delta from the
+    rounded out would show in dq and dk with several roundings' size."""
+    n_ctx, n_groups, k, nh, nkv = shape
+    d = 128
+    at = dict(n_ctx=n_ctx, n_groups=n_groups, k_masks=k)
+    for seed in range(8):
+        q, kk, v, do = attn_inputs(100 + 10 * seed, n_ctx, n_groups, k, nh, nkv, d, BF16, spread=1.5)
+        if odd:
+            buf = torch.empty(v.numel() + 1, dtype=BF16, device="cuda")
+            vv = buf[1:].view(v.shape)
+            v = vv.copy_(v)
+        got = ps.group_attention(q, kk, v, **at)
+        got |= ps.group_attention_backward(do, q, kk, v, got["out"], got["lse"], **at)
+        val, bnd = ref.attention(q, kk, v, do, n_ctx, n_groups, k, d ** -0.5)
+        ref.check(got, val, bnd, ("out", "lse", "dq", "dk", "dv"))
+        for n in ("dq", "dk"):
+            # dS and the result are each rounded once: half a step each, no more than twice that over the whole
+            off = (got[n].double().cpu() - val[n]).norm() / val[n].norm().clamp_min(1e-30)
+            assert off <= 2 * 2.0 ** -8 or val[n].norm() < 1e-6, (n, off.item())

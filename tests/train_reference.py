@@ -72,6 +72,9 @@ def attention(q, k, v, dout, n_ctx, n_groups, k_masks, scale):
             D = (dO * O).sum(-1, keepdim=True)
             eD = (dO.abs() * (eO + d * W * O.abs())).sum(-1, keepdim=True)
             edP = d * W * (dO.abs() @ Vf.abs().T)
+            if u:   # rows of up to 32 keys: delta from the probabilities, not from the rounded out
+                few = (sees.sum(-1, keepdim=True) <= 32)
+                eD = torch.where(few, (P * (edP + (2 * ep + (n + 4) * W) * dP.abs())).sum(-1, keepdim=True), eD)
             dS = P * (dP - D)
             ep2 = 2 * ep + 4 * W
             edS = P * (eD + edP + W * (dP.abs() + D.abs())) * (1 + ep2) + (ep2 + u) * dS.abs()
