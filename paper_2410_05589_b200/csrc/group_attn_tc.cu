@@ -416,7 +416,6 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
     mbar_init(&ctl.o_full, 1);
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    pdl_launch_dependents();
   }
   if (warp == 1) {
     __syncwarp();
@@ -427,6 +426,7 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
   const int i0 = u.i0, i1 = u.i1, rows = u.rows, group = u.group, qrow = u.qrow;
   __syncthreads();
   fence_after_sync();
+  pdl_launch_dependents();   // (with its tensor memory in hand: the next kernel's blocks take theirs before they wait for this one)
   const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_o = tmem + kT;
   volatile int* abort_flag = &ctl.abort_flag;
   pdl_wait();
@@ -708,7 +708,6 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
     mbar_init(&ctl.o_empty, 16);
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    pdl_launch_dependents();
   }
   if (warp == 1) {
     __syncwarp();
@@ -717,6 +716,7 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
   }
   __syncthreads();
   fence_after_sync();
+  pdl_launch_dependents();   // (with its tensor memory in hand: the next kernel's blocks take theirs before they wait for this one)
   const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_dp = tmem + kT, t_o = tmem + 3 * kT;
   volatile int* abort_flag = &ctl.abort_flag;
   const int units = QueryWork::count(s, a, t);
@@ -1225,7 +1225,6 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
     mbar_init(&ctl.o_empty, 16);
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    pdl_launch_dependents();
   }
   if (warp == 1) {
     __syncwarp();
@@ -1234,6 +1233,7 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
   }
   __syncthreads();
   fence_after_sync();
+  pdl_launch_dependents();   // (with its tensor memory in hand: the next kernel's blocks take theirs before they wait for this one)
   const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem, t_dp = tmem + kT, t_dk = tmem + 2 * kT, t_dv = tmem + 3 * kT;
   volatile int* abort_flag = &ctl.abort_flag;
   const int units = KeyWork::count(s, a, t);

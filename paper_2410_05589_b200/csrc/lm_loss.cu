@@ -199,16 +199,17 @@ __global__ void __launch_bounds__(256) k_loss_dx(int H, int splits, int kb, int 
 // ---- products on the FMA units ---------------------------------------------------------------------
 constexpr int kT = 64, kBK = 32, kPitch = 68;
 
-// 64 x 64 tile of A B over k in [k0, k1): 256 threads, thread (ty, tx) has rows 4 ty + i and columns 4 tx + j.  An operand
+// TM x 64 tile of A B over k in [k0, k1): 4 TM threads, thread (ty, tx) has rows 4 ty + i and columns 4 tx + j.  TM is 64, or 32
+// where tiles of 64 would leave multiprocessors without a block (see few_blocks).  An operand
 // is [mn][k] with k contiguous (KC) or [k][mn] with mn contiguous; mn_end: first row (column) that there is none of.  In
 // shared memory both are [k][mn], eight columns' place exchanged by k's bits 3 and 4 so that the transposing stores of
 // a warp (8 rows of 4 groups of k) fall on 32 banks.
-template <bool KC, class T>
-__device__ __forceinline__ void load8(const T* __restrict__ p, size_t ld, int mn0, int mn_end, int k0, int k1, float (&v)[8]) {
-  const int t = threadIdx.x;
+template <bool KC, int TM, class T>
+__device__ __forceinline__ void load8(int t, const T* __restrict__ p, size_t ld, int mn0, int mn_end, int k0, int k1, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = 0.f;
-  const int mn = KC ? mn0 + t / 4 : mn0 + (t % 8) * 8, k = KC ? k0 + (t % 4) * 8 : k0 + t / 8;
+  constexpr int W = TM / 8;   // threads across the tile's width
+  const int mn = KC ? mn0 + t / 4 : mn0 + (t % W) * 8, k = KC ? k0 + (t % 4) * 8 : k0 + t / W;
   const T* q = KC ? p + (size_t)mn * ld + k : p + (size_t)k * ld + mn;
   const int n = KC ? (mn < mn_end ? k1 - k : 0) : (k < k1 ? mn_end - mn : 0);
 #pragma unroll
@@ -223,15 +224,15 @@ __device__ __forceinline__ void load8(const T* __restrict__ p, size_t ld, int mn
     }
   }
 }
-template <bool KC>
-__device__ __forceinline__ void stage8(float* s, const float (&v)[8]) {
-  const int t = threadIdx.x;
+template <bool KC, int TM>
+__device__ __forceinline__ void stage8(int t, float* s, const float (&v)[8]) {
   if (KC) {
     const int mn = (t / 4) ^ ((t % 4) * 8), k = (t % 4) * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[(k + i) * kPitch + mn] = v[i];
   } else {
-    const int k = t / 8, mn = ((t % 8) * 8) ^ (((k >> 3) & 3) * 8);
+    constexpr int W = TM / 8;
+    const int k = t / W, mn = ((t % W) * 8) ^ (((k >> 3) & 3) * 8);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
       *reinterpret_cast<float4*>(s + k * kPitch + mn + 4 * h) = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
@@ -239,7 +240,7 @@ __device__ __forceinline__ void stage8(float* s, const float (&v)[8]) {
 }
 struct TileSmem { float a[kBK * kPitch], b[kBK * kPitch]; };
 
-template <bool AKC, bool BKC>
+template <int TM, bool AKC, bool BKC>
 __device__ __forceinline__ void tile_product(const float* A, size_t lda, int m0, int m_end, const float* B, size_t ldb, int n0,
                                              int n_end, int k0, int k1, TileSmem& sm, float (&c)[4][4]) {
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
@@ -247,18 +248,23 @@ __device__ __forceinline__ void tile_product(const float* A, size_t lda, int m0,
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) c[i][j] = 0.f;
-  float va[8], vb[8];
-  load8<AKC>(A, lda, m0, m_end, k0, k1, va);
-  load8<BKC>(B, ldb, n0, n_end, k0, k1, vb);
+  // (an operand is [mn][k] in eight values a thread: of A's TM columns of k rows that is one set, of B's 64 one or two)
+  constexpr int NB = kT / TM;
+  const int t = threadIdx.x;
+  float va[8], vb[NB][8];
+  auto load = [&](int k) {
+    load8<AKC, TM>(t, A, lda, m0, m_end, k, k1, va);
+#pragma unroll
+    for (int s = 0; s < NB; ++s) load8<BKC, kT>(t + 4 * TM * s, B, ldb, n0, n_end, k, k1, vb[s]);
+  };
+  load(k0);
   for (int k = k0; k < k1; k += kBK) {
     __syncthreads();
-    stage8<AKC>(sm.a, va);
-    stage8<BKC>(sm.b, vb);
+    stage8<AKC, TM>(t, sm.a, va);
+#pragma unroll
+    for (int s = 0; s < NB; ++s) stage8<BKC, kT>(t + 4 * TM * s, sm.b, vb[s]);
     __syncthreads();
-    if (k + kBK < k1) {
-      load8<AKC>(A, lda, m0, m_end, k + kBK, k1, va);
-      load8<BKC>(B, ldb, n0, n_end, k + kBK, k1, vb);
-    }
+    if (k + kBK < k1) load(k + kBK);
 #pragma unroll
     for (int kk = 0; kk < kBK; ++kk) {
       const int sw = ((kk >> 3) & 3) * 8;
@@ -274,15 +280,15 @@ __device__ __forceinline__ void tile_product(const float* A, size_t lda, int m0,
 }
 
 // Logits of a tile -> its rows' maximum and sum (GRAD = false), or g (GRAD = true, vocabulary rows v0 .. v0 + nv).
-template <bool GRAD>
-__global__ void __launch_bounds__(256) k_loss_logits(LossPlan p, LossBuf b, const float* __restrict__ w, int v0, int nv) {
+template <bool GRAD, int TM>
+__global__ void __launch_bounds__(4 * TM) k_loss_logits(LossPlan p, LossBuf b, const float* __restrict__ w, int v0, int nv) {
   __shared__ __align__(16) TileSmem sm;
   pdl_launch_dependents();
   pdl_wait();
-  const int n = *b.n, m0 = blockIdx.y * kT, n0 = blockIdx.x * kT;
+  const int n = *b.n, m0 = blockIdx.y * TM, n0 = blockIdx.x * kT;
   if (m0 >= n) return;
   float c[4][4];
-  tile_product<true, true>((const float*)b.x, p.hidden, m0, n, w + (size_t)v0 * p.hidden, p.hidden, n0, nv, 0, p.hidden, sm, c);
+  tile_product<TM, true, true>((const float*)b.x, p.hidden, m0, n, w + (size_t)v0 * p.hidden, p.hidden, n0, nv, 0, p.hidden, sm, c);
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -319,15 +325,16 @@ __global__ void __launch_bounds__(256) k_loss_logits(LossPlan p, LossBuf b, cons
 }
 
 // dx sums of a piece: rows x hidden, over the piece's vocabulary rows (blockIdx.z: a part of them).
-__global__ void __launch_bounds__(256) k_loss_dx_tile(LossPlan p, LossBuf b, const float* __restrict__ w, int nv, bool add) {
+template <int TM>
+__global__ void __launch_bounds__(4 * TM) k_loss_dx_tile(LossPlan p, LossBuf b, const float* __restrict__ w, int nv, bool add) {
   __shared__ __align__(16) TileSmem sm;
   pdl_launch_dependents();
   pdl_wait();
-  const int n = *b.n, m0 = blockIdx.y * kT, n0 = blockIdx.x * kT;
+  const int n = *b.n, m0 = blockIdx.y * TM, n0 = blockIdx.x * kT;
   if (m0 >= n) return;
   const int per = ((nv + p.splits - 1) / p.splits + 31) / 32 * 32, k0 = min(nv, per * (int)blockIdx.z), k1 = min(nv, k0 + per);
   float c[4][4];
-  tile_product<true, false>((const float*)b.g, p.piece, m0, n, w, p.hidden, n0, p.hidden, k0, k1, sm, c);
+  tile_product<TM, true, false>((const float*)b.g, p.piece, m0, n, w, p.hidden, n0, p.hidden, k0, k1, sm, c);
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -341,13 +348,14 @@ __global__ void __launch_bounds__(256) k_loss_dx_tile(LossPlan p, LossBuf b, con
 }
 
 // dW of a piece: its vocabulary rows x hidden, over the rows.
-__global__ void __launch_bounds__(256) k_loss_dw_tile(LossPlan p, LossBuf b, float* __restrict__ dw, int nv) {
+template <int TM>
+__global__ void __launch_bounds__(4 * TM) k_loss_dw_tile(LossPlan p, LossBuf b, float* __restrict__ dw, int nv) {
   __shared__ __align__(16) TileSmem sm;
   pdl_launch_dependents();
   pdl_wait();
-  const int m0 = blockIdx.y * kT, n0 = blockIdx.x * kT;
+  const int m0 = blockIdx.y * TM, n0 = blockIdx.x * kT;
   float c[4][4];
-  tile_product<false, false>((const float*)b.g, p.piece, m0, nv, (const float*)b.x, p.hidden, n0, p.hidden, 0, *b.n, sm, c);
+  tile_product<TM, false, false>((const float*)b.g, p.piece, m0, nv, (const float*)b.x, p.hidden, n0, p.hidden, 0, *b.n, sm, c);
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -436,15 +444,43 @@ cudaError_t launch_rows(const LossArgs& a, const void* x, size_t ldx, const int*
                       (const float*)(loss ? a.w : nullptr), a.b, vec);
 }
 
+// Whether tiles of 64 rows are fewer than multiprocessors: then tiles of 32, whose steps take half as long (205 rows, 256 x 1000,
+// loss and gradients 98 -> 94 us).
+bool few_blocks(int tiles) { return tiles < device_sms(); }
+
+cudaError_t logits_fp32(const LossArgs& a, bool grad, int v0, int nv, cudaStream_t st) {
+  const LossPlan& p = a.p;
+  const int vt = div_up(nv, kT), mt = div_up(p.rows, kT);
+  const float* w = (const float*)a.w;
+  if (few_blocks(vt * mt)) {
+    const dim3 grid(vt, div_up(p.rows, 32));
+    return grad ? launch_after(k_loss_logits<true, 32>, grid, dim3(128), 0, st, true, p, a.b, w, v0, nv)
+                : launch_after(k_loss_logits<false, 32>, grid, dim3(128), 0, st, true, p, a.b, w, v0, nv);
+  }
+  return grad ? launch_after(k_loss_logits<true, 64>, dim3(vt, mt), dim3(256), 0, st, true, p, a.b, w, v0, nv)
+              : launch_after(k_loss_logits<false, 64>, dim3(vt, mt), dim3(256), 0, st, true, p, a.b, w, v0, nv);
+}
+
 cudaError_t piece_fp32(const LossArgs& a, int v0, int nv, cudaStream_t st) {
   const LossPlan& p = a.p;
   const float* w = (const float*)a.w + (size_t)v0 * p.hidden;
-  const unsigned mt = div_up(p.rows, kT), ht = div_up(p.hidden, kT), vt = div_up(nv, kT);
-  cudaError_t e = launch_after(k_loss_logits<true>, dim3(vt, mt), dim3(256), 0, st, true, p, a.b, (const float*)a.w, v0, nv);
-  if (e == cudaSuccess && a.want_dx)
-    e = launch_after(k_loss_dx_tile, dim3(ht, mt, p.splits), dim3(256), 0, st, true, p, a.b, w, nv, v0 > 0);
-  if (e == cudaSuccess && a.dw)
-    e = launch_after(k_loss_dw_tile, dim3(ht, vt), dim3(256), 0, st, true, p, a.b, (float*)a.dw + (size_t)v0 * p.hidden, nv);
+  float* dw = (float*)a.dw + (size_t)v0 * p.hidden;
+  const unsigned ht = div_up(p.hidden, kT);
+  cudaError_t e = logits_fp32(a, true, v0, nv, st);
+  if (e == cudaSuccess && a.want_dx) {
+    const int mt = div_up(p.rows, kT);
+    if (few_blocks(ht * mt * p.splits))
+      e = launch_after(k_loss_dx_tile<32>, dim3(ht, div_up(p.rows, 32), p.splits), dim3(128), 0, st, true, p, a.b, w, nv, v0 > 0);
+    else
+      e = launch_after(k_loss_dx_tile<64>, dim3(ht, mt, p.splits), dim3(256), 0, st, true, p, a.b, w, nv, v0 > 0);
+  }
+  if (e == cudaSuccess && a.dw) {
+    const int vt = div_up(nv, kT);
+    if (few_blocks(ht * vt))
+      e = launch_after(k_loss_dw_tile<32>, dim3(ht, div_up(nv, 32)), dim3(128), 0, st, true, p, a.b, dw, nv);
+    else
+      e = launch_after(k_loss_dw_tile<64>, dim3(ht, vt), dim3(256), 0, st, true, p, a.b, dw, nv);
+  }
   return e;
 }
 
@@ -479,8 +515,7 @@ extern "C" ps_status ps_lm_loss(int dtype, int rows, int hidden, int vocab, cons
   cudaError_t e = launch_rows(a, x, ldx, labels, nullptr, nullptr, loss, lse, st);
   if (e == cudaSuccess) {
     if (a.p.tc) e = loss_forward_tc(a, st);
-    else
-      e = launch_after(k_loss_logits<false>, dim3(a.p.tiles, div_up(rows, kT)), dim3(256), 0, st, true, a.p, a.b, (const float*)w, 0, vocab);
+    else e = logits_fp32(a, false, 0, vocab, st);
   }
   if (e == cudaSuccess)
     e = launch_after(k_loss_join, dim3(div_up(rows, 8)), dim3(256), 0, st, true, a.p.tiles, a.b, loss, lse);

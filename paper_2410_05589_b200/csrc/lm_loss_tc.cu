@@ -144,7 +144,6 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
     for (int i = 0; i < 2; ++i) { mbar_init(&ctl.acc_full[i], 1); mbar_init(&ctl.acc_empty[i], 2 * kEpiWarps); }
     ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    pdl_launch_dependents();
   }
   __syncwarp();
   // (tensor memory is allocated by the pair together: both run first)
@@ -159,6 +158,7 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
   cluster_wait();
   fence_after_sync();
   if (warp == 1) asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  pdl_launch_dependents();   // (with tensor memory in hand: the next kernel's blocks take theirs before they wait for this one)
   const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem_base;
   volatile int* abort_flag = &ctl.abort_flag;
   pdl_wait();
