@@ -81,25 +81,21 @@ __global__ void __launch_bounds__(1024) k_loss_rows(int rows, int rows_pad, int 
   }
 }
 
-// Compact copy of the rows that count, zeros up to the end of the last tile.  A block per row.  Forward (with w) it also
-// forms the label's logit: the products of the tensor cores truncate as they add (a logit of 1.4 over 5120 terms comes out 1e-5
-// too near zero), which a loss would keep in full while its lse averages it.
+// Row i of the compact copy from row r of x (r < 0: zeros), by a block of 256 threads.  Forward (with w) also the label's
+// logit: the products of the tensor cores truncate as they add (a logit of 1.4 over 5120 terms comes out 1e-5 too near
+// zero), which a loss would keep in full while its lse averages it.
 template <class T>
-__global__ void __launch_bounds__(256) k_loss_gather(int H, int tile, const T* __restrict__ x, size_t ldx, const T* __restrict__ w,
-                                                     LossBuf b, bool vec) {
+__device__ __forceinline__ void take_row(int H, int i, int r, int label, const T* __restrict__ x, size_t ldx, const T* __restrict__ w,
+                                         const LossBuf& b, bool vec) {
   __shared__ float s_sum[8];
-  pdl_launch_dependents();
-  pdl_wait();
-  const int n = *b.n, i = blockIdx.x;
-  if (i >= (n + tile - 1) / tile * tile) return;
   constexpr int N = 16 / sizeof(T);
   uint4* dst = reinterpret_cast<uint4*>((T*)b.x + (size_t)i * H);
-  if (i >= n) {
+  if (r < 0) {
     for (int c = threadIdx.x; c < H / N; c += 256) dst[c] = make_uint4(0, 0, 0, 0);
     return;
   }
-  const T* src = x + (size_t)b.row_of[i] * ldx;
-  const uint4* row = w ? reinterpret_cast<const uint4*>(w + (size_t)b.label[i] * H) : nullptr;
+  const T* src = x + (size_t)r * ldx;
+  const uint4* row = w ? reinterpret_cast<const uint4*>(w + (size_t)label * H) : nullptr;
   float sum = 0.f;
   for (int c = threadIdx.x; c < H / N; c += 256) {
     uint4 v;
@@ -127,6 +123,66 @@ __global__ void __launch_bounds__(256) k_loss_gather(int H, int tile, const T* _
     for (int k = 1; k < 8; ++k) sum += s_sum[k];
     b.picked[i] = sum;
   }
+}
+
+// The compact copy behind k_loss_rows, zeros up to the end of the last tile.  A block per row.
+template <class T>
+__global__ void __launch_bounds__(256) k_loss_gather(int H, int tile, const T* __restrict__ x, size_t ldx, const T* __restrict__ w,
+                                                     LossBuf b, bool vec) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int n = *b.n, i = blockIdx.x;
+  if (i >= (n + tile - 1) / tile * tile) return;
+  const bool in = i < n;
+  take_row<T>(H, i, in ? b.row_of[i] : -1, in ? b.label[i] : -1, x, ldx, w, b, vec);
+}
+
+// Both in one launch for few rows: every block counts the labels itself.  The blocks of rows that do not count, and those beyond
+// the last row, fill up the tile (there are as many of them as compact rows without a row).
+constexpr int kFewRows = 1024;
+template <class T>
+__global__ void __launch_bounds__(256) k_loss_take(int rows, int H, int tile, int V, const int* __restrict__ labels, const T* __restrict__ x,
+                                                   size_t ldx, const T* __restrict__ w, LossBuf b, const float* __restrict__ lse_in,
+                                                   const float* __restrict__ dloss, float* loss, float* lse, bool vec) {
+  __shared__ int s_cnt[2][8];
+  const int tid = threadIdx.x, r = blockIdx.x;
+  pdl_launch_dependents();
+  pdl_wait();
+  int before = 0, n = 0, label = -1;
+#pragma unroll
+  for (int e = 0; e < kFewRows / 256; ++e) {
+    const int k = tid + 256 * e;
+    if (k < rows) {
+      const int l = labels[k];
+      const bool counts = l >= 0 && l < V;
+      n += counts;
+      before += counts && k < r;
+    }
+  }
+  if (r < rows) label = labels[r];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    n += __shfl_xor_sync(0xffffffffu, n, o);
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+  }
+  if ((tid & 31) == 0) { s_cnt[0][tid >> 5] = n; s_cnt[1][tid >> 5] = before; }
+  __syncthreads();
+  n = before = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) { n += s_cnt[0][k]; before += s_cnt[1][k]; }
+  const bool counts = r < rows && label >= 0 && label < V;
+  const int i = counts ? before : n + (r - before);   // (r - before: how many before it do not count)
+  if (tid == 0) {
+    if (r == 0) *b.n = n;
+    if (r < rows) b.slot[r] = counts ? i : -1;
+    b.label[i] = counts ? label : -1;
+    b.lse[i] = counts && lse_in ? lse_in[r] : 0.f;
+    b.up[i] = counts && lse_in ? dloss[r] : 0.f;
+    if (counts) b.row_of[i] = r;
+    else if (loss && r < rows) loss[r] = lse[r] = 0.f;
+  }
+  if (i >= (n + tile - 1) / tile * tile) return;
+  take_row<T>(H, i, counts ? r : -1, label, x, ldx, w, b, vec);
 }
 
 // Joins a row's tiles: a warp per compact row, four tiles a lane in flight.
@@ -429,19 +485,20 @@ ps_status check(const Err& err, int dtype, int rows, int hidden, int vocab, cons
 }
 
 // The rows that count and their compact copy.
+template <class T>
 cudaError_t launch_rows(const LossArgs& a, const void* x, size_t ldx, const int* labels, const float* lse_in,
                         const float* dloss, float* loss, float* lse, cudaStream_t st) {
   const LossPlan& p = a.p;
+  const bool vec = aligned(x, 16) && ldx * sizeof(T) % 16 == 0;
+  const int tile = p.tc ? kLossTile : kT;
+  const T* w = (const T*)(loss ? a.w : nullptr);
+  if (p.rows <= kFewRows)
+    return launch_after(k_loss_take<T>, dim3(p.rows_pad), dim3(256), 0, st, true, p.rows, p.hidden, tile, p.vocab, labels, (const T*)x,
+                        ldx, w, a.b, lse_in, dloss, loss, lse, vec);
   cudaError_t e = launch_after(k_loss_rows, dim3(1), dim3(1024), 0, st, true, p.rows, p.rows_pad, p.vocab, labels, a.b,
                                lse_in, dloss, loss, lse);
   if (e != cudaSuccess) return e;
-  const size_t es = p.tc ? 2 : 4;
-  const bool vec = aligned(x, 16) && ldx * es % 16 == 0;
-  if (p.tc)
-    return launch_after(k_loss_gather<__nv_bfloat16>, dim3(p.rows_pad), dim3(256), 0, st, true, p.hidden, 256,
-                        (const __nv_bfloat16*)x, ldx, (const __nv_bfloat16*)(loss ? a.w : nullptr), a.b, vec);
-  return launch_after(k_loss_gather<float>, dim3(p.rows_pad), dim3(256), 0, st, true, p.hidden, kT, (const float*)x, ldx,
-                      (const float*)(loss ? a.w : nullptr), a.b, vec);
+  return launch_after(k_loss_gather<T>, dim3(p.rows_pad), dim3(256), 0, st, true, p.hidden, tile, (const T*)x, ldx, w, a.b, vec);
 }
 
 // Whether tiles of 64 rows are fewer than multiprocessors: then tiles of 32, whose steps take half as long (205 rows, 256 x 1000,
@@ -512,7 +569,8 @@ extern "C" ps_status ps_lm_loss(int dtype, int rows, int hidden, int vocab, cons
   a.w = w;
   a.status = status ? status : (int*)workspace;
   cudaStream_t st = (cudaStream_t)stream;
-  cudaError_t e = launch_rows(a, x, ldx, labels, nullptr, nullptr, loss, lse, st);
+  cudaError_t e = a.p.tc ? launch_rows<__nv_bfloat16>(a, x, ldx, labels, nullptr, nullptr, loss, lse, st)
+                         : launch_rows<float>(a, x, ldx, labels, nullptr, nullptr, loss, lse, st);
   if (e == cudaSuccess) {
     if (a.p.tc) e = loss_forward_tc(a, st);
     else e = logits_fp32(a, false, 0, vocab, st);
@@ -545,7 +603,8 @@ extern "C" ps_status ps_lm_loss_backward(int dtype, int rows, int hidden, int vo
   if (ps_status s = check_workspace(err, "ps_lm_loss_backward", workspace, workspace_bytes, a.b.bytes)) return s;
   a.w = w; a.dw = dw; a.want_dx = dx != nullptr;
   a.status = status ? status : (int*)workspace;
-  cudaError_t e = launch_rows(a, x, ldx, labels, lse, dloss, nullptr, nullptr, st);
+  cudaError_t e = a.p.tc ? launch_rows<__nv_bfloat16>(a, x, ldx, labels, lse, dloss, nullptr, nullptr, st)
+                         : launch_rows<float>(a, x, ldx, labels, lse, dloss, nullptr, nullptr, st);
   for (int v0 = 0; e == cudaSuccess && v0 < vocab; v0 += a.p.piece) {
     const int nv = std::min(a.p.piece, vocab - v0);
     e = a.p.tc ? loss_piece_tc(a, v0, nv, st) : piece_fp32(a, v0, nv, st);
