@@ -6,6 +6,7 @@ library is missing or no CUDA device is present, calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import threading
@@ -212,23 +213,26 @@ def verify_static(draft_tokens: torch.Tensor, draft_logits, target_logits: torch
 _DTYPE_CODE = {torch.float32: PS_DTYPE_F32, torch.bfloat16: PS_DTYPE_BF16}
 
 
-class _on:
-    """Makes the tensors' device current, and ``stream`` where one is given."""
-
-    def __init__(self, device, stream):
-        self.ctx = []
-        if device.index is not None and device.index != _device():
-            self.ctx.append(torch.cuda.device(device))
-        if stream is not None:
-            self.ctx.append(torch.cuda.stream(stream))
-
+class _Here:
     def __enter__(self):
-        for c in self.ctx:
-            c.__enter__()
+        pass
 
     def __exit__(self, *exc):
-        for c in reversed(self.ctx):
-            c.__exit__(*exc)
+        pass
+
+
+_HERE = _Here()
+
+
+def _on(device, stream):
+    """Makes the tensors' device current, and ``stream`` where one is given."""
+    if stream is None and device.index == _device():
+        return _HERE
+    both = contextlib.ExitStack()
+    both.enter_context(torch.cuda.device(device))
+    if stream is not None:
+        both.enter_context(torch.cuda.stream(stream))
+    return both
 
 
 # (What these checks cost on the host is most of what a small call costs: texts are put together only for a refusal, a
@@ -259,6 +263,8 @@ def _first(t, name):
 
 def _rows(t, width, name):
     """Row stride in elements of a tensor of rows that are dense; a view of a wider buffer may have a larger one."""
+    if t.is_contiguous() and t.numel() == width * t.shape[0]:
+        return width
     shape, stride = t.shape, t.stride()
     w = 1
     for i in range(len(shape) - 1, 0, -1):
@@ -293,6 +299,10 @@ def _ptr(t):
 
 def _scratch(nbytes, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None   # (0: the call says why)
+
+
+def _dense_like(t):
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _group_args(q, k, v, n_ctx, n_groups, k_masks, scale):
@@ -333,7 +343,7 @@ def group_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_ctx, n_
     with _on(device, stream):
         o = out if out is not None else {}
         if "out" not in o:
-            o["out"] = torch.empty(q.shape, dtype=q.dtype, device=device)
+            o["out"] = _dense_like(q)
         if "lse" not in o:
             o["lse"] = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=device)
         y, lse = o["out"], o["lse"]
@@ -360,7 +370,7 @@ def group_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tenso
         o = grads if grads is not None else {}
         for name, like in (("dq", q), ("dk", k), ("dv", v)):
             if name not in o:
-                o[name] = torch.empty(like.shape, dtype=q.dtype, device=device)
+                o[name] = _dense_like(like)
             elif o[name].shape != like.shape:
                 _refuse(f"{name} has another shape than its tensor")
         dq, dk, dv = o["dq"], o["dk"], o["dv"]
@@ -433,7 +443,7 @@ def lm_loss_backward(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, lse
         o = grads if grads is not None else {}
         for name, like, want in (("dx", x, want_dx), ("dw", w, want_dw)):
             if want and name not in o:
-                o[name] = torch.empty(like.shape, dtype=x.dtype, device=device)
+                o[name] = _dense_like(like)
         dx, dw = o.get("dx") if want_dx else None, o.get("dw") if want_dw else None
         _tensors(device, dx, dw, dtype=x.dtype)
         _tensors(device, lse, dloss, status)
