@@ -384,7 +384,7 @@ __device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const Q
       for (int e = 0; e < D / 32; ++e) o[e] = fmaf(p, y[e], o[e]);
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : m + logf(l);
+  const float inv = l == 0.f && t.splits > 1 ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : m + logf(l);   // (see the kernel)
   if (t.splits == 1) {
     bf16* dst = (bf16*)a.out + row_q * a.ldo + (size_t)h * D;
 #pragma unroll
@@ -556,7 +556,9 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
     if (ok && i0 < i1) ok = all_sync(mbar_wait(&ctl.o_full, 0, abort_flag));
     if (ok) {
       fence_after_sync();
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      // (no sum: a part of the keys of which the row sees none leaves zeros, which the join passes over; a row whose scores
+      // are all -inf has no probabilities, and its zeros times 1/0 are no number)
+      const float inv = l == 0.f && t.splits > 1 ? 0.f : 1.f / l;
       const size_t row = (size_t)qrow + r, at = ((size_t)u.split * a.n_heads + u.h) * a.rows + row;
       bf16* dst = (bf16*)a.out + row * a.ldo + (size_t)u.h * D;
       float odd = l * 0.f;                   // no number once a sum is not finite
