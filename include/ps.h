@@ -456,7 +456,8 @@ ps_status ps_group_attn_backward(const ps_group_attn_args* a, void* workspace, s
 
 /* Softmax cross entropy of the LM head, forward and backward, over pieces of the vocabulary: the logits
  * x w^T (in single precision) never exist as a whole.
- *   lse_i = log sum_v exp(x_i . w_v),  loss_i = lse_i - x_i . w_label(i)
+ *   lse_i = log sum_v exp(x_i . w_v),  loss_i = lse_i - x_i . w_label(i) (not formed as that difference: it is never below
+ *   zero, and as exact relatively where the label has nearly all of the probability)
  *   g_iv = dloss_i (exp(x_i . w_v - lse_i) - [v = label(i)]),  dx_i = sum_v g_iv w_v,  dw_v = sum_i g_iv x_i
  * A row whose label lies outside [0, vocab) (such as -100) counts for nothing: its loss, lse and dx are
  * 0, it adds nothing to dw, and neither its x nor its dloss is read.

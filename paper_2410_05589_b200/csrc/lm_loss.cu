@@ -3,7 +3,9 @@
 //   s = x W^T,  lse = log sum_v exp s_v,  loss = lse - s_label
 //   g = dloss (exp(s - lse) - onehot),    dx = g W,  dW = g^T x
 // Forward: each tile of the product x W^T leaves, per row, the maximum of its logits and the sum of their
-// exponentials against it; a small kernel joins the tiles.  Backward:
+// exponentials against it, without the label's; a small kernel joins the tiles to r = log sum_{v != label} exp s_v and
+// forms loss = log(1 + exp(r - s_label)).  (As lse - s_label, the difference of near numbers, the loss of a row that the head
+// is sure of was what the two were off by: 1e-5 below zero where it is 1e-10.)  Backward:
 // the logits of a piece of the vocabulary are formed again, turned into g by the epilogue of the product
 // that forms them and kept for the two products that use them.  dx is summed over the pieces in single
 // precision, dW of a piece is complete.
@@ -83,7 +85,7 @@ __global__ void __launch_bounds__(1024) k_loss_rows(int rows, int rows_pad, int 
 
 // Row i of the compact copy from row r of x (r < 0: zeros), by a block of 256 threads.  Forward (with w) also the label's
 // logit: the products of the tensor cores truncate as they add (a logit of 1.4 over 5120 terms comes out 1e-5 too near
-// zero), which a loss would keep in full while its lse averages it.
+// zero), which a loss would keep in full while the others' sum averages it.
 template <class T>
 __device__ __forceinline__ void take_row(int H, int i, int r, int label, const T* __restrict__ x, size_t ldx, const T* __restrict__ w,
                                          const LossBuf& b, bool vec) {
@@ -216,10 +218,13 @@ __global__ void __launch_bounds__(256) k_loss_join(int tiles, LossBuf b, float* 
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (__any_sync(0xffffffffu, nan)) s = NAN;
   if (lane == 0) {
-    const float l = top + logf(s);
+    // s has all but the label's logit (vocab = 1: nothing).  lse is that of the logits as the product formed them, which the
+    // backward call forms again; the loss takes the label's in single precision.
+    const float rest = top + logf(s), own = b.own[i], picked = b.picked[i], high = fmaxf(own, rest);
+    const float d = rest - picked, e = log1pf(expf(-fabsf(d)));
     const int r = b.row_of[i];
-    lse[r] = l;
-    loss[r] = l - b.picked[i];
+    lse[r] = high == -INFINITY && own == rest ? high : high + log1pf(expf(-fabsf(own - rest)));
+    loss[r] = picked == INFINITY ? NAN : (d > 0.f ? d + e : e);     // (inf - inf: no number, like every other logit of +inf)
   }
 }
 
@@ -360,10 +365,15 @@ __global__ void __launch_bounds__(4 * TM) k_loss_logits(LossPlan p, LossBuf b, c
           ((float*)b.g)[(size_t)m * p.piece + v] = up * (exp2f((c[i][j] - l) * kLog2e) - (v == label ? 1.f : 0.f));
       }
     } else {
+      const int label = in ? b.label[m] : -1;
       float top = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int v = n0 + 4 * tx + j;
+        if (v == label) {
+          b.own[m] = c[i][j];
+          c[i][j] = -INFINITY;
+        }
         if (v < nv) top = fmaxf(top, c[i][j]);
       }
 #pragma unroll
@@ -462,6 +472,7 @@ LossBuf carve(void* ws, const LossPlan& p, bool backward) {
   b.x = c.take<char>((size_t)p.rows_pad * p.hidden * es);
   if (!backward) {
     b.part = c.take<float2>((size_t)p.tiles * p.rows_pad);
+    b.own = c.take<float>(p.rows_pad);
     b.picked = c.take<float>(p.rows_pad);
   } else {
     b.g = c.take<char>((size_t)p.rows_pad * p.piece * es);

@@ -14,9 +14,10 @@ struct LossBuf {
   int* label;            // [rows_pad] of compact rows
   float *lse, *up;       // [rows_pad] of compact rows: lse and dloss (backward)
   void* x;               // [rows_pad][hidden] compact rows, dtype
-  // forward: per vocabulary tile and compact row the maximum and the sum of exponentials against it
+  // forward: per vocabulary tile and compact row the maximum and the sum of exponentials against it, the label's logit left out
   float2* part;          // [rows_pad][tiles]
-  float* picked;         // [rows_pad] logit of the label
+  float* own;            // [rows_pad] logit of the label as the product formed it
+  float* picked;         // [rows_pad] logit of the label in single precision
   // backward
   void* g;               // [rows_pad][piece] gradient of a piece's logits
   float* acc;            // [splits][rows_pad][hidden] dx so far

@@ -1,6 +1,6 @@
 // Products of the LM-head loss on the 5th-generation tensor cores (bf16 operands, fp32 sums):
 //
-//   forward   S = X W^T  -> per row and half tile: maximum, sum of exponentials
+//   forward   S = X W^T  -> per row and half tile: maximum and sum of exponentials of all but the label's logit; that one
 //   gradient  S = X W^T  -> G = up (exp(S - lse) - onehot), rounded to bf16 (the operand type of the two products
 //                           that read it; what they add up is fp32)
 //   dx        G W        -> sums over the pieces in fp32, a piece in up to four parts of its k (see dx_splits)
@@ -239,10 +239,11 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
       const int buf = c & 1;
       int mt, nt, part;
       place(t, mt, nt, part);
+      const int m = mt * kTile + (int)rank * 128 + r, c0 = nt * kTile + half * 128;
+      const int own = MODE == FWD ? a.b.label[m] - c0 : -1;   // the label's column of these 128
       const bool ok = kb == 0 || mbar_wait(&ctl.acc_full[buf], (c >> 1) & 1, abort_flag);
       if (!__all_sync(0xffffffffu, ok)) break;
       fence_after_sync();
-      const int m = mt * kTile + (int)rank * 128 + r, c0 = nt * kTile + half * 128;
       const uint32_t ta = tmem + ((uint32_t)(32 * q) << 16) + buf * kTile + half * 128;
       if (MODE == FWD) {
         float top = -INFINITY, sum = 0.f;
@@ -251,6 +252,14 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
           float v[32];
           tmem_ld32(ta + j0, v);
           const int left = a.cols - c0 - j0;
+          if (__any_sync(0xffffffffu, own >= j0 && own < j0 + 32)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j0 + j == own) {
+                a.b.own[m] = v[j];
+                v[j] = -INFINITY;
+              }
+          }
           float mx = top;
 #pragma unroll
           for (int j = 0; j < 32; ++j) {

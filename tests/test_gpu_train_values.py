@@ -1,4 +1,5 @@
-"""Values that a diverging training step meets: what is not finite shows where it is met."""
+"""Values that a diverging or a finished training step meets: what is not finite shows where it is met; losses of rows that the
+head is sure of."""
 import math
 
 import pytest
@@ -42,3 +43,67 @@ def test_row_whose_scores_are_all_minus_infinity_is_no_number(ps, n_ctx, n_group
     good = torch.ones(q.shape[0], dtype=torch.bool, device="cuda")
     good[bad] = False
     assert torch.isfinite(r["out"][good]).all() and torch.isfinite(r["lse"][:, good]).all() and torch.isfinite(r["dq"][good]).all()
+
+
+# ---- rows that the head is sure of ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("H, V, logit", [(4096, 1500, 30.0), (1024, 32000, 40.0), (256, 700, 18.0), (64, 1, 5.0), (2048, 257, 60.0)])
+@TYPES
+def test_loss_of_rows_that_the_head_is_sure_of(ps, H, V, logit, dtype):
+    """The label's logit far above the others: loss = log(1 + sum_v exp(s_v - s_label)) is as small as that, and never below zero.
+
+    With d = log sum_{v != label} exp(s_v) - s_label the loss is log(1 + e^d), whose slope e^d / (1 + e^d) is the others' share of
+    the probability.  So it may be off by that share of what d is off by (two scores, a sum, an fp32 logarithm and a
+    difference of numbers of its parts' size), and by its own roundings."""
+    rows = 70
+    w = normal(1, (V, H), 0.02, dtype)
+    g = torch.Generator().manual_seed(2)
+    labels = torch.randint(0, V, (rows,), generator=g, dtype=torch.int32)
+    labels[:3] = torch.tensor([0, V - 1, V // 2], dtype=torch.int32)
+    own = w[labels.long().cuda()].float()
+    x = (own * (logit / own.square().sum(-1, keepdim=True))).to(dtype)
+    labels = labels.cuda()
+    got = ps.lm_loss(x, w, labels)
+    S = x.double().cpu() @ w.double().cpu().T
+    lab = labels.long().cpu()
+    elem = torch.arange(rows)
+    es = (H + 8) * ref.W * (x.double().cpu().abs() @ w.double().cpu().abs().T).amax(-1)
+    own_s = S[elem, lab].clone()
+    S[elem, lab] = -math.inf
+    d = torch.logsumexp(S, -1) - own_s
+    want = torch.nn.functional.softplus(d)
+    share = torch.sigmoid(d)
+    ed = 2 * es + (V + 8) * ref.W + 8 * ref.W * (torch.logsumexp(S, -1).abs().nan_to_num(0, 0, 0) + own_s.abs())
+    loss = got["loss"].double().cpu()
+    assert (loss >= 0).all(), loss.min().item()
+    off = (loss - want).abs()
+    assert (off <= share * ed * (1 + ed) + 8 * ref.W * want).all(), (off.max().item(), want.max().item())
+    lse = torch.logaddexp(torch.logsumexp(S, -1), own_s)
+    assert ((got["lse"].double().cpu() - lse).abs() <= es + (V + 8) * ref.W + 8 * ref.W * lse.abs()).all()
+
+
+@TYPES
+def test_loss_of_extreme_logits(ps, dtype):
+    """A label's logit of -inf, of +inf or that is no number, and others of +inf or -inf."""
+    V, H = 300, 64
+    w = normal(3, (V, H), 0.1, dtype)
+    w[:, :4] = 0
+    w[7, 0], w[8, 1], w[:, 2], w[9, 3] = 1.0, 1.0, 1.0, math.nan
+    x = normal(4, (6, H), 1.0, dtype)
+    x[:, :4] = 0
+    # rows of which one logit alone is not finite need a w that is: huge products instead of infinite operands
+    big = 2.0 ** 127
+    x[0, 0], w[7, 0] = big, -2.0     # the label's logit is -inf
+    x[1, 0] = -big                   # ... +inf
+    x[2, 1], w[8, 1] = big, 2.0      # another one is +inf
+    x[3, 1] = -big                   # ... -inf: nothing but one term less
+    x[4, 2], w[:, 2] = -big, 2.0     # all of them are -inf
+    x[5, 2] = 0
+    w[9, 3] = 0
+    labels = torch.tensor([7, 7, 5, 5, 5, 5], dtype=torch.int32, device="cuda")
+    loss = ps.lm_loss(x, w, labels)["loss"].double().cpu()
+    assert loss[0] == math.inf and torch.isnan(loss[[1, 4]]).all() and not torch.isfinite(loss[2])
+    S = x[[3, 5]].double().cpu() @ w.double().cpu().T
+    want = torch.logsumexp(torch.where(S < -3e38, -math.inf, S), -1) - S[:, 5]
+    # (72 roundings of 2^-23 of a sum of 64 products of about 0.06: 3.4e-5 at most for a score, twice that for their difference)
+    assert ((loss[[3, 5]] - want).abs() <= 1e-4).all()
