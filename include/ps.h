@@ -423,7 +423,9 @@ ps_status ps_verify_static(int vocab, int B, int n_draft, int n_target, const in
  *   dq_r = scale sum_c ds_rc k_c,  dk_c = scale sum_r ds_rc q_r
  * where a key head's sums run over all query heads that share it.  q and k are as they are after the
  * rotation (row j of group t stands at position n_ctx + t + j).  The backward pass forms p again from q, k and lse.
- * A key or value that a row does not see does not touch that row, whatever its bits are.
+ * A key or value that a row does not see does not touch that row, whatever its bits are (bf16: rows and keys that share a tile
+ * with a value that is not finite are formed again one by one, which may take some ten times as long as the call otherwise
+ * does; a tensor that is NaN throughout costs little).
  * Rows are [heads][head_dim], dense within a row; any row stride of at least that width. */
 typedef struct ps_group_attn_args {
   int dtype;            /* PS_DTYPE_* */

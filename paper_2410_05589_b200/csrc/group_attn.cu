@@ -488,6 +488,7 @@ size_t carve(void* ws, const Seqs& s, const ps_group_attn_args* a, bool backward
   if (a->dtype != PS_DTYPE_BF16) return c.at;
   t->gpt = tk->gpt = groups_per_tile(128, s.R);
   t->splits = attn_splits(s, a->n_heads, backward);
+  t->none = t->splits > 1 ? 0.f : NAN;
   const size_t parts_q = t->splits > 1 ? units * t->splits * a->head_dim : 0;
   size_t parts_k = 0;
   if (backward) {
@@ -497,6 +498,14 @@ size_t carve(void* ws, const Seqs& s, const ps_group_attn_args* a, bool backward
   // (dq's parts are joined before dk and dv are formed)
   t->part_o = tk->part_o = c.take<float>(std::max(parts_q, parts_k));
   t->part_l = c.take<float>(t->splits > 1 && !backward ? units * t->splits : 0);
+  if (backward) {
+    t->lots = attn_lots(s, a->n_heads);
+    g->any = c.take<int>(1);
+    t->bad = c.take<uint32_t>((size_t)t->lots * 16 * t->splits);
+    t->where = c.take<Where>((size_t)t->lots * 4);
+    tk->bad = c.take<uint32_t>((size_t)tk->key_units * 32);
+    tk->where = c.take<Where>((size_t)tk->lots * 4);
+  }
   return c.at;
 }
 

@@ -36,6 +36,7 @@ struct AttnArgs {
   void *dq, *dk, *dv;
   size_t lddq, lddk, lddv;
   float* delta;              // [n_heads][rows] dout . out
+  int* any;                  // bf16, backward: whether a sum is not finite
   int* status;
 };
 

@@ -17,7 +17,9 @@
 // tiles: the scores are formed twice in the backward pass, and no sum depends on the order of atomics.
 //
 // A product of a probability of zero and a value that is not finite is not zero.  A row of sums that holds
-// a value that is not finite is therefore formed again, by one warp, over what the row sees alone.
+// a value that is not finite is therefore formed again, by one warp, over what the row sees alone: in the forward kernel by the
+// block that has it, behind its last wait; in the backward pass by a kernel of its own (k_gat_again), since the persistent
+// blocks' next units wait, within bounds, for the warps that would do it.
 // Every wait is bounded: on expiry the kernel raises the status word and returns.
 #include "group_attn_tc.cuh"
 #include "umma_gemm.cuh"
@@ -292,17 +294,63 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-template <int D>
-__device__ __forceinline__ void lane_load(const bf16* p, int lane, float (&x)[D / 32]) {
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) x[i] = __bfloat162float(p[lane + 32 * i]);
+// C = D / 32 neighbouring channels of a row, bf16: a lane's part of it.
+template <int C>
+struct Chans { uint32_t v[C / 2]; };
+template <int C>
+__device__ __forceinline__ Chans<C> chan_load(const bf16* p) {
+  Chans<C> r;
+  if constexpr (C == 8) {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    r.v[0] = x.x; r.v[1] = x.y; r.v[2] = x.z; r.v[3] = x.w;
+  } else if constexpr (C == 4) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    r.v[0] = x.x; r.v[1] = x.y;
+  } else {
+    r.v[0] = *reinterpret_cast<const uint32_t*>(p);
+  }
+  return r;
 }
-template <int D>
-__device__ __forceinline__ float lane_dot(const float (&x)[D / 32], const float (&y)[D / 32]) {
+template <int C>
+__device__ __forceinline__ void chan_store(bf16* p, const float (&x)[C]) {
+  if constexpr (C == 8)
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+  else if constexpr (C == 4) *reinterpret_cast<uint2*>(p) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+  else *reinterpret_cast<uint32_t*>(p) = pack2(x[0], x[1]);
+}
+template <int C>
+__device__ __forceinline__ float chan(const Chans<C>& x, int e) {
+  return __uint_as_float(e % 2 ? x.v[e / 2] & 0xFFFF0000u : x.v[e / 2] << 16);
+}
+template <int C>
+__device__ __forceinline__ float chan_dot(const Chans<C>& x, const Chans<C>& y) {
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) s = fmaf(x[i], y[i], s);
-  return warp_sum(s);
+  for (int e = 0; e < C; ++e) s = fmaf(chan(x, e), chan(y, e), s);
+  return s;
+}
+// Whether every lane's sums have become no number, which further terms do not change.
+template <int C>
+__device__ __forceinline__ bool all_nan(const float (&x)[C]) {
+  bool nan = true;
+#pragma unroll
+  for (int e = 0; e < C; ++e) nan &= x[e] != x[e];
+  return all_sync(nan);
+}
+// A walk over [begin, end): kWalk rows together, whose loads and sums over the lanes then overlap; `on` is asked after each of those.
+constexpr int kWalk = 8;
+template <class Row, class On>
+__device__ __forceinline__ bool walk(int begin, int end, Row row, On on) {
+  for (int i0 = begin; i0 < end; i0 += kWalk) {
+    if (i0 + kWalk <= end) {
+#pragma unroll
+      for (int i = 0; i < kWalk; ++i) row(i0 + i);
+    } else {
+      for (int i = i0; i < end; ++i) row(i);
+    }
+    if (!on()) return false;
+  }
+  return true;
 }
 
 // Unit of a persistent block's round: every other round backwards, so that no block has the longest unit of each.
@@ -350,51 +398,37 @@ struct FwdCtl {
   int abort_flag;
 };
 
-// Row r of the query tile over its key tiles [i0, i1), by one warp and over the keys it sees alone.
+// out of row r of the query tile over its key tiles [i0, i1), by one warp and over the keys it sees alone (their lse is there).
 template <int D>
 __device__ __noinline__ void fwd_row(const AttnArgs& a, const TcArgs& t, const QueryWork u, int r) {
+  constexpr int C = D / 32;
   const int lane = threadIdx.x & 31, h = u.h;
-  const size_t row_q = (size_t)u.qrow + r;
+  const size_t row_q = (size_t)u.qrow + r, at = ((size_t)u.split * a.n_heads + h) * a.rows + row_q;
+  const float lse = t.splits == 1 ? a.lse[at] : t.part_l[at];
   const TileRow tr(r, u.w.R);
-  const bf16 *k = (const bf16*)a.k + (size_t)(h / a.per) * D, *v = (const bf16*)a.v + (size_t)(h / a.per) * D;
-  float q[D / 32], o[D / 32], m = -INFINITY, l = 0.f;
-  lane_load<D>((const bf16*)a.q + row_q * a.ldq + (size_t)h * D, lane, q);
+  const bf16 *k = (const bf16*)a.k + (size_t)(h / a.per) * D + C * lane, *v = (const bf16*)a.v + (size_t)(h / a.per) * D + C * lane;
+  const Chans<C> q = chan_load<C>((const bf16*)a.q + row_q * a.ldq + (size_t)h * D + C * lane);
+  float o[C];
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-  for (int i = u.i0; i < u.i1; ++i) {
+  for (int e = 0; e < C; ++e) o[e] = 0.f;
+  bool on = lse > -INFINITY;   // (else this part of the keys has none that counts)
+  for (int i = u.i0; on && i < u.i1; ++i) {
     int x0, n, lo, hi;
     const int kind = u.w.tile(i, u.group, u.rows, x0, n);
     tr.sees(kind, x0, n, u.group, u.rows, lo, hi);
-    for (int c = lo; c <= hi; ++c) {
+    on = walk(lo, hi + 1, [&](int c) {
       const size_t row = u.w.key_row(kind, x0 + c);
-      float kx[D / 32], y[D / 32];
-      lane_load<D>(k + row * a.ldk, lane, kx);
-      lane_load<D>(v + row * a.ldv, lane, y);
-      const float sc = lane_dot<D>(q, kx) * a.scale;
-      if (sc > m) {
-        const float f = m > -INFINITY ? exp2f((m - sc) * kLog2e) : 0.f;
-        l *= f;
+      const Chans<C> x = chan_load<C>(k + row * a.ldk), y = chan_load<C>(v + row * a.ldv);
+      const float p = exp2f((warp_sum(chan_dot(q, x)) * a.scale - lse) * kLog2e);
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) o[e] *= f;
-        m = sc;
-      }
-      const float p = exp2f((sc - (m > -INFINITY ? m : 0.f)) * kLog2e);
-      l += p;
-#pragma unroll
-      for (int e = 0; e < D / 32; ++e) o[e] = fmaf(p, y[e], o[e]);
-    }
+      for (int e = 0; e < C; ++e) o[e] = fmaf(p, chan(y, e), o[e]);
+    }, [&] { return !all_nan(o); });
   }
-  const float inv = l == 0.f && t.splits > 1 ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : m + logf(l);   // (see the kernel)
   if (t.splits == 1) {
-    bf16* dst = (bf16*)a.out + row_q * a.ldo + (size_t)h * D;
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * inv);
-    if (lane == 0) a.lse[(size_t)h * a.rows + row_q] = lse;
+    chan_store<C>((bf16*)a.out + row_q * a.ldo + (size_t)h * D + C * lane, o);
   } else {
-    const size_t at = ((size_t)u.split * a.n_heads + h) * a.rows + row_q;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) t.part_o[at * D + lane + 32 * e] = o[e] * inv;
-    if (lane == 0) t.part_l[at] = lse;
+    for (int e = 0; e < C; ++e) t.part_o[at * D + C * lane + e] = o[e];
   }
 }
 
@@ -557,11 +591,11 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
     if (ok) {
       fence_after_sync();
       // (no sum: a part of the keys of which the row sees none leaves zeros, which the join passes over; a row whose scores
-      // are all -inf has no probabilities, and its zeros times 1/0 are no number)
-      const float inv = l == 0.f && t.splits > 1 ? 0.f : 1.f / l;
+      // are all -inf has no probabilities, and is no number)
+      const float inv = l == 0.f ? t.none : 1.f / l;
       const size_t row = (size_t)qrow + r, at = ((size_t)u.split * a.n_heads + u.h) * a.rows + row;
       bf16* dst = (bf16*)a.out + row * a.ldo + (size_t)u.h * D;
-      float odd = l * 0.f;                   // no number once a sum is not finite
+      float odd = 0.f;                       // no number once a sum is not finite
 #pragma unroll
       for (int j = 0; j < D; j += 32) {
         uint32_t o[32];
@@ -593,7 +627,8 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
         if (t.splits == 1) a.lse[(size_t)u.h * a.rows + row] = lse;
         else t.part_l[at] = lse;
       }
-      unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f);
+      // (where l is no number, or a row has none, all of it is no number, and so it came out)
+      unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f && inv == inv);
       __syncwarp();
       for (; bad; bad &= bad - 1) fwd_row<D>(a, t, u, 32 * q + __ffs(bad) - 1);
     }
@@ -649,43 +684,6 @@ struct DqCtl {
   uint32_t tmem;
   int abort_flag;
 };
-
-// A quarter of the columns of row r of the query tile, by one warp and over the keys the row sees alone.
-template <int D>
-__device__ __noinline__ void dq_row(const AttnArgs& a, const TcArgs& t, const QueryWork u, int r, int quarter) {
-  const int lane = threadIdx.x & 31, h = u.h;
-  const size_t row_q = (size_t)u.qrow + r;
-  const TileRow tr(r, u.w.R);
-  const bf16 *k = (const bf16*)a.k + (size_t)(h / a.per) * D, *v = (const bf16*)a.v + (size_t)(h / a.per) * D;
-  float q[D / 32], g[D / 32], o[D / 32];
-  lane_load<D>((const bf16*)a.q + row_q * a.ldq + (size_t)h * D, lane, q);
-  lane_load<D>((const bf16*)a.dout + row_q * a.lddo + (size_t)h * D, lane, g);
-  const float lse = a.lse[(size_t)h * a.rows + row_q], delta = a.delta[(size_t)h * a.rows + row_q];
-#pragma unroll
-  for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-  for (int i = u.i0; i < u.i1; ++i) {
-    int x0, n, lo, hi;
-    const int kind = u.w.tile(i, u.group, u.rows, x0, n);
-    tr.sees(kind, x0, n, u.group, u.rows, lo, hi);
-    for (int c = lo; c <= hi; ++c) {
-      const size_t row = u.w.key_row(kind, x0 + c);
-      float x[D / 32], y[D / 32];
-      lane_load<D>(k + row * a.ldk, lane, x);
-      lane_load<D>(v + row * a.ldv, lane, y);
-      const float p = exp2f((lane_dot<D>(q, x) * a.scale - lse) * kLog2e), ds = p * (lane_dot<D>(g, y) - delta);
-#pragma unroll
-      for (int e = 0; e < D / 32; ++e) o[e] = fmaf(ds, x[e], o[e]);
-    }
-  }
-  float* part = t.part_o + (((size_t)u.split * a.n_heads + h) * a.rows + row_q) * D;
-  bf16* dst = (bf16*)a.dq + row_q * a.lddq + (size_t)h * D;
-#pragma unroll
-  for (int e = 0; e < D / 32; ++e) {
-    if ((lane + 32 * e) / (D / 4) != quarter) continue;
-    if (t.splits > 1) part[lane + 32 * e] = o[e] * a.scale;
-    else dst[lane + 32 * e] = __float2bfloat16_rn(o[e] * a.scale);
-  }
-}
 
 template <int D>
 __global__ void __launch_bounds__(Dq<D>::threads, 1)
@@ -880,9 +878,16 @@ k_gat_dq(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, cons
           for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(part + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
         }
       }
-      unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f);
-      __syncwarp();
-      for (; bad; bad &= bad - 1) dq_row<D>(a, t, u, 32 * q + __ffs(bad) - 1, quarter);
+      // (where lse or delta is no number, the whole row is, and so it came out)
+      const unsigned bad = __ballot_sync(0xffffffffu, r < rows && odd != 0.f && lse == lse && delta == delta);
+      if (lane == 0) {
+        const int at_unit = units - 1 - unit, lot = 4 * (at_unit / t.splits) + q;
+        t.bad[4 * ((size_t)lot * t.splits + at_unit % t.splits) + quarter] = bad;
+        if (bad) {
+          t.where[lot] = Where{u.qrow + 32 * q, 1, u.h};
+          *a.any = 1;
+        }
+      }
     }
     fence_before_sync();
   }
@@ -915,41 +920,6 @@ __global__ void __launch_bounds__(256) k_gat_dq_join(const __grid_constant__ Att
 // channels; it also forms delta = dout . out of the rows it reads anyway.
 // Measured: 6650 rows of 40 heads 110 us (409 MB, 3.7 TB/s); 10235 rows of 32 heads on 8, 89 us.  Bound by the latency of a
 // warp's loads: its registers leave room for 12 warps an SM (with spills at 16 and 20 it took 129 and 136 us).
-template <int C>
-struct Chans { uint32_t v[C / 2]; };   // C neighbouring channels, bf16
-template <int C>
-__device__ __forceinline__ Chans<C> chan_load(const bf16* p) {
-  Chans<C> r;
-  if constexpr (C == 8) {
-    const uint4 x = *reinterpret_cast<const uint4*>(p);
-    r.v[0] = x.x; r.v[1] = x.y; r.v[2] = x.z; r.v[3] = x.w;
-  } else if constexpr (C == 4) {
-    const uint2 x = *reinterpret_cast<const uint2*>(p);
-    r.v[0] = x.x; r.v[1] = x.y;
-  } else {
-    r.v[0] = *reinterpret_cast<const uint32_t*>(p);
-  }
-  return r;
-}
-template <int C>
-__device__ __forceinline__ void chan_store(bf16* p, const float (&x)[C]) {
-  if constexpr (C == 8)
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
-  else if constexpr (C == 4) *reinterpret_cast<uint2*>(p) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
-  else *reinterpret_cast<uint32_t*>(p) = pack2(x[0], x[1]);
-}
-template <int C>
-__device__ __forceinline__ float chan(const Chans<C>& x, int e) {
-  return __uint_as_float(e % 2 ? x.v[e / 2] & 0xFFFF0000u : x.v[e / 2] << 16);
-}
-template <int C>
-__device__ __forceinline__ float chan_dot(const Chans<C>& x, const Chans<C>& y) {
-  float s = 0.f;
-#pragma unroll
-  for (int e = 0; e < C; ++e) s = fmaf(chan(x, e), chan(y, e), s);
-  return s;
-}
-
 // delta of the rows with few keys (see kExactKeys): the first groups of sequences with a short context.  A warp per (row, head).
 __host__ __device__ inline int few_groups(int ctx, int groups) { return ctx >= kExactKeys ? 0 : (groups < kExactKeys - ctx ? groups : kExactKeys - ctx); }
 template <int D>
@@ -995,6 +965,7 @@ k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, 
   pdl_wait();
   const int lane = threadIdx.x % 32, R = s.R;
   const long long unit = (long long)blockIdx.x * 4 + threadIdx.x / 32;
+  if (unit == 0 && lane == 0) *a.any = 0;   // (for the kernels behind this one)
   if (unit >= (long long)groups * a.n_kv) return;
   const int g = (int)(unit / a.n_kv), hk = (int)(unit - (long long)g * a.n_kv);
   int lo = 0, hi = s.B - 1;            // the sequence of group g: its rows begin at q0 / R
@@ -1157,50 +1128,6 @@ struct KeyWork {
   }
 };
 
-// Quarter of the columns of dk and dv of key i of the tile, by one warp and over the rows that see it alone.
-template <int D>
-__device__ __noinline__ void dkv_row(const Seqs& s, const AttnArgs& a, const TcArgs& t, const KeyWork u, int i, int quarter) {
-  const int lane = threadIdx.x & 31;
-  const size_t row = (size_t)u.row0 + (size_t)i * u.step;
-  float k[D / 32], v[D / 32], dk[D / 32], dv[D / 32];
-  lane_load<D>((const bf16*)a.k + row * a.ldk + (size_t)u.hk * D, lane, k);
-  lane_load<D>((const bf16*)a.v + row * a.ldv + (size_t)u.hk * D, lane, v);
-#pragma unroll
-  for (int e = 0; e < D / 32; ++e) dk[e] = dv[e] = 0.f;
-  int lo, hi;
-  u.seen(i, s.R, lo, hi);
-  KeyWork::Step x(u, a.per);
-  for (int j = u.j0; j < u.j1; ++j, x.next()) {
-    const int h = x.h, r0 = x.r0;
-    for (int r = max(lo, r0); r <= min(hi, r0 + kT - 1); ++r) {
-      const size_t qr = (size_t)s.q0[u.b] + r;
-      float q[D / 32], g[D / 32];
-      lane_load<D>((const bf16*)a.q + qr * a.ldq + (size_t)h * D, lane, q);
-      lane_load<D>((const bf16*)a.dout + qr * a.lddo + (size_t)h * D, lane, g);
-      const float p = exp2f((lane_dot<D>(q, k) * a.scale - a.lse[(size_t)h * a.rows + qr]) * kLog2e);
-      const float ds = p * (lane_dot<D>(g, v) - a.delta[(size_t)h * a.rows + qr]);
-#pragma unroll
-      for (int e = 0; e < D / 32; ++e) {
-        dv[e] = fmaf(p, g[e], dv[e]);
-        dk[e] = fmaf(ds, q[e], dk[e]);
-      }
-    }
-  }
-  bf16 *ok = (bf16*)a.dk + row * a.lddk + (size_t)u.hk * D, *ov = (bf16*)a.dv + row * a.lddv + (size_t)u.hk * D;
-  float* part = t.part_o + ((size_t)u.slot * 2 * kT + i) * D;
-#pragma unroll
-  for (int e = 0; e < D / 32; ++e) {
-    if ((lane + 32 * e) / (D / 4) != quarter) continue;
-    if (u.parts > 1) {
-      part[lane + 32 * e] = dk[e] * a.scale;
-      part[kT * D + lane + 32 * e] = dv[e];
-    } else {
-      ok[lane + 32 * e] = __float2bfloat16_rn(dk[e] * a.scale);
-      ov[lane + 32 * e] = __float2bfloat16_rn(dv[e]);
-    }
-  }
-}
-
 template <int D>
 __global__ void __launch_bounds__(Dkv<D>::threads, 1)
 k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a,
@@ -1358,7 +1285,12 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
     for (int round = 0, unit; ok && (unit = unit_of(round), round * (int)gridDim.x < units); ++round) {
       if (unit >= units) continue;
       const KeyWork u(s, a, t, unit);
-      if (!u.there()) continue;
+      const int lot = 4 * (unit / t.parts) + q;
+      uint32_t* bad_out = t.bad + 8 * ((size_t)lot * t.parts + unit % t.parts) + 2 * quarter;
+      if (!u.there()) {
+        if (lane == 0) bad_out[0] = bad_out[1] = 0;
+        continue;
+      }
       const int cnt = u.j1 - u.j0;
       int see0, see1;
       u.seen(key, s.R, see0, see1);
@@ -1425,11 +1357,10 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
       const bool in = key < u.n;
       const size_t row = (size_t)u.row0 + (size_t)key * u.step;
       float* part = t.part_o + ((size_t)u.slot * 2 * kT + key) * D + N * quarter;
-      float odd = 0.f;
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         uint32_t x[N];
-        float y[N];
+        float y[N], odd = 0.f;
         if (cnt > 0) {
           ldn<N>((kv ? t_dv : t_dk) + lanes + N * quarter, x);
           ld_wait();
@@ -1456,10 +1387,15 @@ k_gat_dkv(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
               *reinterpret_cast<float4*>(part + kv * kT * D + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
           }
         }
+        const unsigned bad = __ballot_sync(0xffffffffu, in && odd != 0.f);
+        if (lane == 0) {
+          bad_out[kv] = bad;
+          if (bad) {
+            t.where[lot] = Where{u.row0 + 32 * q * u.step, u.step, u.hk};
+            *a.any = 1;
+          }
+        }
       }
-      unsigned bad = __ballot_sync(0xffffffffu, in && odd != 0.f);
-      __syncwarp();
-      for (; bad; bad &= bad - 1) dkv_row<D>(s, a, t, u, 32 * q + __ffs(bad) - 1, quarter);
     }
     fence_before_sync();
   }
@@ -1488,6 +1424,105 @@ __global__ void __launch_bounds__(256) k_gat_dkv_join(const __grid_constant__ Se
         for (int e = 0; e < D / 32; ++e) x[e] += part[((size_t)p * 2 + kv) * kT * D + e];
       chan_store<D / 32>((kv ? (bf16*)a.dv + row * a.lddv : (bf16*)a.dk + row * a.lddk) + (size_t)u.hk * D + (D / 32) * lane, x);
     }
+  }
+}
+
+// ---- backward: sums that are not finite --------------------------------------------------------------------
+// dq of the rows, dk and dv of the keys that k_gat_dq and k_gat_dkv left a bit for, over what the row sees (what sees the key)
+// alone, by a warp each.  Sums that have become no number in every column end the walk, so that a step that is NaN throughout costs
+// little more than another.  What costs is a value that reaches rows or keys by its place in a tile alone, or a part of
+// the columns.  Measured (2047 groups of 5 rows, 32 heads on 8; forward and backward 0.24 + 0.77 ms): all of dout, q or k NaN
+// 0.24 + 0.87, all of v 1.1 + 0.87; one NaN early in dout or q 0.24 + 17 (119 keys a head over all 40940 rows), in v 22 +
+// 0.85 (all rows over all keys), in k 0.24 + 0.84.  Without one this launch takes 2 us.
+template <int D>
+__device__ __noinline__ void row_again(const Seqs& s, const AttnArgs& a, int qr, int h) {
+  constexpr int C = D / 32;
+  int lo = 0, hi = s.B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (s.q0[mid] <= qr) lo = mid; else hi = mid - 1;
+  }
+  const int lane = threadIdx.x & 31, R = s.R, ctx = s.ctx[lo], rho = qr - s.q0[lo], t = rho / R, n = ctx + t + 1 + rho % R;
+  const size_t kv0 = s.kv0[lo], g0 = kv0 + ctx;
+  const bf16 *k = (const bf16*)a.k + (size_t)(h / a.per) * D + C * lane, *v = (const bf16*)a.v + (size_t)(h / a.per) * D + C * lane;
+  const Chans<C> q = chan_load<C>((const bf16*)a.q + (size_t)qr * a.ldq + (size_t)h * D + C * lane),
+                 g = chan_load<C>((const bf16*)a.dout + (size_t)qr * a.lddo + (size_t)h * D + C * lane);
+  const float lse = a.lse[(size_t)h * a.rows + qr], delta = a.delta[(size_t)h * a.rows + qr];
+  float o[C];
+#pragma unroll
+  for (int e = 0; e < C; ++e) o[e] = 0.f;
+  walk(0, n, [&](int c) {
+    const size_t row = c < ctx ? kv0 + c : (c <= ctx + t ? g0 + (size_t)(c - ctx) * R : g0 + (size_t)t * R + (c - ctx - t));
+    const Chans<C> x = chan_load<C>(k + row * a.ldk), y = chan_load<C>(v + row * a.ldv);
+    const float p = exp2f((warp_sum(chan_dot(q, x)) * a.scale - lse) * kLog2e), ds = p * (warp_sum(chan_dot(g, y)) - delta);
+#pragma unroll
+    for (int e = 0; e < C; ++e) o[e] = fmaf(ds, chan(x, e), o[e]);
+  }, [&] { return !all_nan(o); });
+#pragma unroll
+  for (int e = 0; e < C; ++e) o[e] *= a.scale;
+  chan_store<C>((bf16*)a.dq + (size_t)qr * a.lddq + (size_t)h * D + C * lane, o);
+}
+template <int D>
+__device__ __noinline__ void key_again(const Seqs& s, const AttnArgs& a, int kr, int hk, bool want_k, bool want_v) {
+  constexpr int C = D / 32;
+  int lo = 0, hi = s.B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (s.kv0[mid] <= kr) lo = mid; else hi = mid - 1;
+  }
+  const int lane = threadIdx.x & 31, R = s.R, ctx = s.ctx[lo], x = kr - s.kv0[lo];
+  const int r_begin = x < ctx ? 0 : (x - ctx) / R * R, r_end = s.groups[lo] * R;
+  const Chans<C> k = chan_load<C>((const bf16*)a.k + (size_t)kr * a.ldk + (size_t)hk * D + C * lane),
+                 v = chan_load<C>((const bf16*)a.v + (size_t)kr * a.ldv + (size_t)hk * D + C * lane);
+  float dk[C], dv[C];
+#pragma unroll
+  for (int e = 0; e < C; ++e) dk[e] = dv[e] = 0.f;
+  bool on = true;
+  for (int h = hk * a.per; on && h < (hk + 1) * a.per; ++h) {
+    const bf16 *q_in = (const bf16*)a.q + (size_t)h * D + C * lane, *g_in = (const bf16*)a.dout + (size_t)h * D + C * lane;
+    const float *lse = a.lse + (size_t)h * a.rows, *delta = a.delta + (size_t)h * a.rows;
+    on = walk(r_begin, r_end, [&](int r) {
+      const size_t qr = (size_t)s.q0[lo] + r;
+      const Chans<C> q = chan_load<C>(q_in + qr * a.ldq), g = chan_load<C>(g_in + qr * a.lddo);
+      const float p = exp2f((warp_sum(chan_dot(q, k)) * a.scale - lse[qr]) * kLog2e), ds = p * (warp_sum(chan_dot(g, v)) - delta[qr]);
+#pragma unroll
+      for (int e = 0; e < C; ++e) {
+        dv[e] = fmaf(p, chan(g, e), dv[e]);
+        dk[e] = fmaf(ds, chan(q, e), dk[e]);
+      }
+    }, [&] { return (want_k && !all_nan(dk)) || (want_v && !all_nan(dv)); });
+  }
+#pragma unroll
+  for (int e = 0; e < C; ++e) dk[e] *= a.scale;
+  if (want_k) chan_store<C>((bf16*)a.dk + (size_t)kr * a.lddk + (size_t)hk * D + C * lane, dk);
+  if (want_v) chan_store<C>((bf16*)a.dv + (size_t)kr * a.lddv + (size_t)hk * D + C * lane, dv);
+}
+template <int D>
+__global__ void __launch_bounds__(256) k_gat_again(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a,
+                                                   const __grid_constant__ TcArgs tq, const __grid_constant__ TcArgs tk) {
+  pdl_launch_dependents();
+  pdl_wait();
+  if (*a.any == 0) return;
+  const int keys = s.kv0[s.B];
+  for (long long i = blockIdx.x; i < 16 * (tq.lots + tk.lots); i += gridDim.x) {
+    const bool of_keys = i >= 16 * tq.lots;
+    const TcArgs& t = of_keys ? tk : tq;
+    const long long lot = (of_keys ? i - 16 * tq.lots : i) / 4;
+    uint32_t bad[2] = {0, 0};
+    if (of_keys) {
+      for (int e = 0; e < 8 * tk.parts; ++e) bad[e & 1] |= tk.bad[lot * 8 * tk.parts + e];
+    } else {
+      for (int e = 0; e < 4 * tq.splits; ++e) bad[0] |= tq.bad[lot * 4 * tq.splits + e];
+    }
+    const int e = 8 * (int)(i & 3) + (threadIdx.x >> 5);
+    const uint32_t bit = 1u << e;
+    if (!((bad[0] | bad[1]) & bit)) continue;
+    const Where w = t.where[lot];
+    // (after a wait that ran out the words are whatever memory held)
+    const long long row = w.row + (long long)e * w.step;
+    if (row < 0 || row >= (of_keys ? keys : a.rows) || w.head < 0 || w.head >= (of_keys ? a.n_kv : a.n_heads)) continue;
+    if (of_keys) key_again<D>(s, a, (int)row, w.head, bad[0] & bit, bad[1] & bit);
+    else row_again<D>(s, a, (int)row, w.head);
   }
 }
 
@@ -1583,8 +1618,10 @@ cudaError_t backward(const Maps& maps, const Seqs& s0, const AttnArgs& a, const 
   Seqs s = sorted(s0, true);
   const long long tiles = key_tiles(s), works = tiles * a.n_kv * tk.parts;
   e = launch_after(k_gat_dkv<D>, dim3((unsigned)std::min<long long>(works, sms)), dim3(Dkv<D>::threads), Dkv<D>::smem, st, true, maps, s, a, tk);
-  if (e != cudaSuccess || tk.parts == 1) return e;
-  return launch_after(k_gat_dkv_join<D>, dim3((unsigned)(tiles * a.n_kv), kT / 16), dim3(256), 0, st, true, s, a, tk);
+  if (e == cudaSuccess && tk.parts > 1)
+    e = launch_after(k_gat_dkv_join<D>, dim3((unsigned)(tiles * a.n_kv), kT / 16), dim3(256), 0, st, true, s, a, tk);
+  if (e != cudaSuccess || a.rows == 0) return e;
+  return launch_after(k_gat_again<D>, dim3(2 * sms), dim3(256), 0, st, true, s0, a, tq, tk);
 }
 
 }  // namespace
@@ -1607,6 +1644,11 @@ void attn_parts(const Seqs& s, int n_kv, int per, TcArgs* t) {
   t->parts = units == 0 ? 1 : (int)std::max<long long>(1, std::min<long long>(std::min<long long>(kParts, 4ll * device_sms() / units), steps / 4));
   t->cap = std::max(1, div_up(steps, t->parts));
   t->key_units = units * t->parts;
+  t->lots = units;
+}
+long long attn_lots(const Seqs& s, int n_heads) {
+  Seqs c = s;
+  return (long long)query_tiles(c) * n_heads;
 }
 
 bool attn_tc_takes(const AttnArgs& a, bool backward) {

@@ -1,5 +1,5 @@
-"""Values that a diverging or a finished training step meets: what is not finite shows where it is met; losses of rows that the
-head is sure of."""
+"""Values that a diverging or a finished training step meets: what is not finite shows where it is met and nowhere else, and at
+no other cost to the call; losses of rows that the head is sure of."""
 import math
 
 import pytest
@@ -107,3 +107,69 @@ def test_loss_of_extreme_logits(ps, dtype):
     want = torch.logsumexp(torch.where(S < -3e38, -math.inf, S), -1) - S[:, 5]
     # (72 roundings of 2^-23 of a sum of 64 products of about 0.06: 3.4e-5 at most for a score, twice that for their difference)
     assert ((loss[[3, 5]] - want).abs() <= 1e-4).all()
+
+
+# ---- a step that has diverged -----------------------------------------------------------------------------------
+
+def times(fn, n):
+    fn()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    for _ in range(n):
+        fn()
+    b.record()
+    torch.cuda.synchronize()
+    return a.elapsed_time(b) / n
+
+
+@pytest.mark.parametrize("where", ["do", "v", "k", "q"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_attention_of_a_step_that_has_diverged(ps, where, bad):
+    """One tensor without a finite value: every wait ends as it does otherwise, every value that meets it says so, and the call takes
+    no longer by an order of magnitude (a row that is no number is not formed again)."""
+    n_ctx, n_groups, k, nh, nkv, d = [300, 0], [500, 430], 4, 8, 2, 64
+    q, kk, v, do = attn_inputs(71, n_ctx, n_groups, k, nh, nkv, d, BF16)
+    at = dict(n_ctx=n_ctx, n_groups=n_groups, k_masks=k)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def run():
+        r = ps.group_attention(q, kk, v, status=status, **at)
+        return r | ps.group_attention_backward(do, q, kk, v, r["out"], r["lse"], status=status, **at)
+
+    fine = times(run, 5)
+    {"do": do, "v": v, "k": kk, "q": q}[where].fill_(bad)
+    r = run()
+    for n in ("dq", "dk") + (() if where == "v" else ("dv",)) + (() if where == "do" else ("out",)):
+        assert not torch.isfinite(r[n]).any(), n
+    assert status.item() == 0
+    if math.isnan(bad):
+        diverged = times(run, 2)
+        assert diverged <= 10 * fine + 1.0, (fine, diverged)
+
+
+@pytest.mark.parametrize("where", ["do", "v", "k", "q"])
+def test_a_diverged_sequence_leaves_its_neighbours_alone(ps, where):
+    """Tiles at the end of a sequence reach into the next one's rows: what is not finite there comes to nothing, for every key and
+    row of the sequence, at one warp a row over the whole device."""
+    n_ctx, n_groups, k, nh, nkv, d = [130, 20, 65], [90, 70, 61], 4, 4, 2, 64
+    R = k + 1
+    q, kk, v, do = attn_inputs(73, n_ctx, n_groups, k, nh, nkv, d, BF16)
+    val, bnd = ref.attention(q, kk, v, do, n_ctx, n_groups, k, d ** -0.5)
+    q0, k0 = n_groups[0] * R, n_ctx[0] + n_groups[0] * R
+    q1, k1 = q0 + n_groups[1] * R, k0 + n_ctx[1] + n_groups[1] * R
+    t = {"do": do, "v": v, "k": kk, "q": q}[where]
+    t[(slice(k0, k1) if where in "kv" else slice(q0, q1))] = math.nan
+    at = dict(n_ctx=n_ctx, n_groups=n_groups, k_masks=k)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    r = ps.group_attention(q, kk, v, status=status, **at)
+    r |= ps.group_attention_backward(do, q, kk, v, r["out"], r["lse"], status=status, **at)
+    assert status.item() == 0
+    for n in ("out", "dq", "dk", "dv"):
+        lo, hi = (k0, k1) if n in ("dk", "dv") else (q0, q1)
+        off = (r[n].double().cpu() - val[n]).abs() <= bnd[n] + 1e-30
+        assert off[:lo].all() and off[hi:].all(), n
+        if n == "dq" or (n == "out" and where != "do"):
+            assert torch.isnan(r[n][lo:hi]).all(), n
+    off = (r["lse"].double().cpu() - val["lse"]).abs() <= bnd["lse"] + 1e-30
+    assert off[:, :q0].all() and off[:, q1:].all()
