@@ -406,10 +406,21 @@ ps_status ps_verify_static(int vocab, int B, int n_draft, int n_target, const in
  *     between a row's width and its stride, are left as they are.
  *   - results do not depend on what else runs, nor from one run to the next.
  *   - status   device [1] int or NULL: bit 1 is OR-ed in when a bounded device-side wait expired and
- *              the outputs are not to be used (the caller zeroes it beforehand)
+ *              the outputs are not to be used (the caller zeroes it beforehand).  NULL: the library's own word
+ *              of the device, which ps_train_poll reads
  *   - err      host buffer for an error text, or NULL;  err_cap its size in bytes
  *   - workspace device memory of at least the *_workspace_bytes() of the same sizes, 256-byte
  *              aligned (PS_ERR_CAPACITY if smaller, PS_ERR_INVALID_ARG if misaligned) */
+
+/* Waits for `stream`, then returns and clears what calls on the current device without a status word of their own have
+ * reported: PS_OK, or PS_ERR_TIMEOUT if a bounded device-side wait of any of them has expired since it was last asked (their
+ * outputs are not to be used).  PS_ERR_INVALID_ARG while `stream` is captured. */
+ps_status ps_train_poll(void* stream);
+
+/* Test helper for that path: enqueues a one-thread kernel whose wait on a barrier that nothing completes gives up after
+ * `limit_cycles` clock cycles (at most 4e9) and is reported as the kernels of the attention (loss = 0) or of the loss
+ * (loss = 1) report theirs, to `status` or, if it is NULL, to the library's word. */
+ps_status ps_debug_train_wait_expires(int loss, long long limit_cycles, int* status, void* stream);
 
 /* Attention under the mask of parallel groups, forward and backward (the mask of ps_group_forward).
  * B sequences lie one behind the other.  Sequence b has n_ctx[b] context positions, which lend
@@ -424,8 +435,8 @@ ps_status ps_verify_static(int vocab, int B, int n_draft, int n_target, const in
  * where a key head's sums run over all query heads that share it.  q and k are as they are after the
  * rotation (row j of group t stands at position n_ctx + t + j).  The backward pass forms p again from q, k and lse.
  * A key or value that a row does not see does not touch that row, whatever its bits are (bf16: rows and keys that share a tile
- * with a value that is not finite are formed again one by one, which may take some ten times as long as the call otherwise
- * does; a tensor that is NaN throughout costs little).
+ * with a value that is not finite are formed again one by one, which may take up to a hundred times as long as the call
+ * otherwise does; a tensor that is NaN throughout costs little).
  * Rows are [heads][head_dim], dense within a row; any row stride of at least that width. */
 typedef struct ps_group_attn_args {
   int dtype;            /* PS_DTYPE_* */

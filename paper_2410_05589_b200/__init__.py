@@ -18,6 +18,7 @@ from .binding import (  # noqa: F401
     lm_loss_backward,
     load_library,
     philox_fill,
+    train_poll,
     verify_static,
 )
 from .build import build  # noqa: F401

@@ -37,6 +37,7 @@ EXPORTS = (
     "ps_debug_gemm_plan", "ps_debug_append_pass_rows",
     "ps_group_attn_workspace_bytes", "ps_group_attn", "ps_group_attn_backward", "ps_lm_loss_workspace_bytes",
     "ps_lm_loss", "ps_lm_loss_backward", "ps_embed_rows", "ps_embed_rows_workspace_bytes", "ps_embed_rows_backward",
+    "ps_train_poll", "ps_debug_train_wait_expires",
 )
 
 
@@ -134,6 +135,8 @@ def load_library(path: str | None = None) -> C.CDLL:
     lib.ps_embed_rows_workspace_bytes.restype = sz
     lib.ps_embed_rows_workspace_bytes.argtypes = [C.c_int] * 5
     lib.ps_embed_rows_backward.argtypes = [C.c_int] * 5 + [vp, f, vp, sz, vp, vp, vp, sz, C.c_char_p, sz, vp]
+    lib.ps_train_poll.argtypes = [vp]
+    lib.ps_debug_train_wait_expires.argtypes = [C.c_int, C.c_longlong, vp, vp]
     _lib = lib
     return lib
 
@@ -210,6 +213,8 @@ def verify_static(draft_tokens: torch.Tensor, draft_logits, target_logits: torch
 # ---- training operators ----------------------------------------------------------------------------
 # Functions of tensors: they need no Drafter.  Outputs and workspaces are allocated per call on the stream the
 # call runs on (pass ``out`` to reuse outputs), so that calls on several streams and captured graphs share nothing.
+# ``status`` (int32, zeroed by the caller) has bit 1 set by a call whose device-side wait expired; calls without one report to
+# a word of the device that ``train_poll`` reads.
 _DTYPE_CODE = {torch.float32: PS_DTYPE_F32, torch.bfloat16: PS_DTYPE_BF16}
 
 
@@ -301,6 +306,20 @@ def _scratch(nbytes, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None   # (0: the call says why)
 
 
+def _check_status(status, device):
+    if status is not None:
+        _tensors(device, status, dtype=torch.int32)
+        if status.numel() < 1:
+            _refuse("status [1] int32")
+
+
+def train_poll(device=None) -> int:
+    """ps_train_poll: waits for the device's current stream and returns (and clears) what calls there without ``status`` have
+    reported: PS_OK, or PS_ERR_TIMEOUT if a bounded wait of any of them expired, whose outputs are not to be used."""
+    with torch.cuda.device(device):
+        return load_library().ps_train_poll(_stream())
+
+
 def _dense_like(t):
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
@@ -348,7 +367,8 @@ def group_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_ctx, n_
             o["lse"] = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=device)
         y, lse = o["out"], o["lse"]
         _tensors(device, y, dtype=q.dtype)
-        _tensors(device, lse, status)
+        _tensors(device, lse)
+        _check_status(status, device)
         _check_lse(lse, q)
         if y.shape != q.shape:
             _refuse("out has another shape than q")
@@ -375,7 +395,8 @@ def group_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tenso
                 _refuse(f"{name} has another shape than its tensor")
         dq, dk, dv = o["dq"], o["dk"], o["dv"]
         _tensors(device, dout, out, dq, dk, dv, dtype=q.dtype)
-        _tensors(device, lse, status)
+        _tensors(device, lse)
+        _check_status(status, device)
         _check_lse(lse, q)
         if dout.shape != q.shape or out.shape != q.shape:
             _refuse("dout and out have the shape of q")
@@ -422,7 +443,8 @@ def lm_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, out: dict | 
             if name not in o:
                 o[name] = torch.empty(x.shape[0], dtype=torch.float32, device=device)
         loss, lse = o["loss"], o["lse"]
-        _tensors(device, loss, lse, status)
+        _tensors(device, loss, lse)
+        _check_status(status, device)
         _check_rows_of_floats(labels, loss=loss, lse=lse)
         n = lib.ps_lm_loss_workspace_bytes(*size, 0)
         ws = _scratch(n, device)
@@ -446,7 +468,8 @@ def lm_loss_backward(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, lse
                 o[name] = _dense_like(like)
         dx, dw = o.get("dx") if want_dx else None, o.get("dw") if want_dw else None
         _tensors(device, dx, dw, dtype=x.dtype)
-        _tensors(device, lse, dloss, status)
+        _tensors(device, lse, dloss)
+        _check_status(status, device)
         _check_rows_of_floats(labels, lse=lse, dloss=dloss)
         if dx is not None and dx.shape != x.shape:
             _refuse("dx has another shape than x")

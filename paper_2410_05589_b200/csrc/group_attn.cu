@@ -536,7 +536,7 @@ ps_status run(const ps_group_attn_args* a, bool backward, void* workspace, size_
   g.out = a->out; g.ldo = a->ldo; g.lse = a->lse;
   g.dout = a->dout; g.lddo = a->lddo;
   g.dq = a->dq; g.dk = a->dk; g.dv = a->dv; g.lddq = a->lddq; g.lddk = a->lddk; g.lddv = a->lddv;
-  g.status = status ? status : (int*)workspace;
+  g.status = status;
   const bool f32 = a->dtype == PS_DTYPE_F32, d64 = a->head_dim == 64;
   cudaError_t e;
   if (!f32 && attn_tc_takes(g, backward))

@@ -22,6 +22,7 @@
 // blocks' next units wait, within bounds, for the warps that would do it.
 // Every wait is bounded: on expiry the kernel raises the status word and returns.
 #include "group_attn_tc.cuh"
+#include "train_status.cuh"
 #include "umma_gemm.cuh"
 
 namespace ps {
@@ -364,7 +365,7 @@ __device__ __forceinline__ void finish(int tid, int warp, volatile int* abort_fl
   __syncthreads();
   if (*abort_flag) {
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);   // (copies and MMAs in flight)
-    if (tid == 0) atomicOr(status, kStatTimeout);
+    if (tid == 0) report_timeout(status);
     __syncthreads();
   }
   if (warp == 1) {
@@ -1671,6 +1672,9 @@ cudaError_t attn_tc(int D, bool backward_, const Seqs& s, const AttnArgs& a, con
   if (backward_) return D == 64 ? backward<64>(m, s, a, t, tk, st) : backward<128>(m, s, a, t, tk, st);
   return D == 64 ? forward<64>(m, s, a, t, st) : forward<128>(m, s, a, t, st);
 }
+
+cudaError_t attn_take_status(int* word, cudaStream_t st) { return take_word(word, st); }
+cudaError_t attn_wait_expires(long long limit, int* status, cudaStream_t st) { return wait_expires(limit, status, st); }
 
 }  // namespace train
 }  // namespace ps

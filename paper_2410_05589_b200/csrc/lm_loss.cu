@@ -578,7 +578,7 @@ extern "C" ps_status ps_lm_loss(int dtype, int rows, int hidden, int vocab, cons
   a.b = carve(workspace, a.p, false);
   if (ps_status s = check_workspace(err, "ps_lm_loss", workspace, workspace_bytes, a.b.bytes)) return s;
   a.w = w;
-  a.status = status ? status : (int*)workspace;
+  a.status = status;
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e = a.p.tc ? launch_rows<__nv_bfloat16>(a, x, ldx, labels, nullptr, nullptr, loss, lse, st)
                          : launch_rows<float>(a, x, ldx, labels, nullptr, nullptr, loss, lse, st);
@@ -613,7 +613,7 @@ extern "C" ps_status ps_lm_loss_backward(int dtype, int rows, int hidden, int vo
   a.b = carve(workspace, a.p, true);
   if (ps_status s = check_workspace(err, "ps_lm_loss_backward", workspace, workspace_bytes, a.b.bytes)) return s;
   a.w = w; a.dw = dw; a.want_dx = dx != nullptr;
-  a.status = status ? status : (int*)workspace;
+  a.status = status;
   cudaError_t e = a.p.tc ? launch_rows<__nv_bfloat16>(a, x, ldx, labels, lse, dloss, nullptr, nullptr, st)
                          : launch_rows<float>(a, x, ldx, labels, lse, dloss, nullptr, nullptr, st);
   for (int v0 = 0; e == cudaSuccess && v0 < vocab; v0 += a.p.piece) {

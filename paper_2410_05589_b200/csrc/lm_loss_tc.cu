@@ -21,6 +21,7 @@
 // sustains.  Up to 256 rows one tile of rows takes the vocabulary at 6.2 TB/s.  Warp 0 issues the TMA loads, warp 1 the MMAs (of the pair: in the leader CTA), warps
 // 2..9 read the sums back.  Every wait is bounded: on expiry the kernel raises the status word and returns.
 #include "lm_loss.cuh"
+#include "train_status.cuh"
 #include "umma_gemm.cuh"
 
 namespace ps {
@@ -355,7 +356,7 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
   if (ctl.abort_flag) {
     // let copies and MMAs that are still in flight finish before shared and tensor memory go
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);
-    if (tid == 0) atomicOr(a.status, kStatTimeout);
+    if (tid == 0) report_timeout(a.status);
     __syncthreads();
   }
   cluster_arrive();
@@ -426,6 +427,9 @@ cudaError_t loss_piece_tc(const LossArgs& a, int v0, int nv, cudaStream_t st) {
   }
   return e;
 }
+
+cudaError_t loss_take_status(int* word, cudaStream_t st) { return take_word(word, st); }
+cudaError_t loss_wait_expires(long long limit, int* status, cudaStream_t st) { return wait_expires(limit, status, st); }
 
 }  // namespace train
 }  // namespace ps

@@ -51,3 +51,29 @@ ps_status check_workspace(const Err& err, const char* who, const void* ws, size_
 
 }  // namespace train
 }  // namespace ps
+
+using namespace ps::train;
+
+extern "C" ps_status ps_train_poll(void* stream) {
+  cudaStream_t st = (cudaStream_t)stream;
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(st, &capture) == cudaSuccess && capture != cudaStreamCaptureStatusNone) return PS_ERR_INVALID_ARG;
+  int words[2] = {0, 0};
+  cudaError_t e = attn_take_status(&words[0], st);
+  if (e == cudaSuccess) e = loss_take_status(&words[1], st);
+  const cudaError_t done = cudaStreamSynchronize(st);   // (whatever failed: the words must not be written once they are gone)
+  if (e != cudaSuccess || done != cudaSuccess) {
+    (void)cudaGetLastError();
+    return PS_ERR_CUDA;
+  }
+  return (words[0] | words[1]) & ps::kStatTimeout ? PS_ERR_TIMEOUT : PS_OK;
+}
+
+extern "C" ps_status ps_debug_train_wait_expires(int loss, long long limit_cycles, int* status, void* stream) {
+  if (limit_cycles < 0 || limit_cycles > 4000000000LL) return PS_ERR_INVALID_ARG;
+  const cudaError_t e = loss ? loss_wait_expires(limit_cycles, status, (cudaStream_t)stream)
+                             : attn_wait_expires(limit_cycles, status, (cudaStream_t)stream);
+  if (e == cudaSuccess) return PS_OK;
+  (void)cudaGetLastError();
+  return PS_ERR_CUDA;
+}

@@ -33,7 +33,7 @@ int device_sms();
 // Lets `kern` have `bytes` of dynamic shared memory on the current device; `done`: one word per kernel, a bit per device.
 cudaError_t allow_smem(const void* kern, int bytes, std::atomic<uint64_t>& done);
 
-// Slices of a workspace, one behind the other; the first kAlign bytes are the status word of calls without one.
+// Slices of a workspace, one behind the other (behind kAlign bytes, so that none is empty: 0 bytes mean sizes that are refused).
 struct Carve {
   char* base;
   size_t at = kAlign;
@@ -45,6 +45,11 @@ struct Carve {
     return p;
   }
 };
+// What a wait that ran out leaves in the words of calls without one of their own (train_status.cuh), and one that does.
+cudaError_t attn_take_status(int* word, cudaStream_t st);
+cudaError_t loss_take_status(int* word, cudaStream_t st);
+cudaError_t attn_wait_expires(long long limit, int* status, cudaStream_t st);
+cudaError_t loss_wait_expires(long long limit, int* status, cudaStream_t st);
 ps_status check_workspace(const Err& err, const char* who, const void* ws, size_t have, size_t need);
 
 }  // namespace train
