@@ -214,7 +214,8 @@ def verify_static(draft_tokens: torch.Tensor, draft_logits, target_logits: torch
 # Functions of tensors: they need no Drafter.  Outputs and workspaces are allocated per call on the stream the
 # call runs on (pass ``out`` to reuse outputs), so that calls on several streams and captured graphs share nothing.
 # ``status`` (int32, zeroed by the caller) has bit 1 set by a call whose device-side wait expired; calls without one report to
-# a word of the device that ``train_poll`` reads.
+# a word of the device that ``train_poll`` reads.  With ``stream`` the caller orders it behind what wrote the inputs, and keeps
+# inputs and outputs until it is done with them, as with any tensor that is used on another stream than its own.
 _DTYPE_CODE = {torch.float32: PS_DTYPE_F32, torch.bfloat16: PS_DTYPE_BF16}
 
 
@@ -230,9 +231,13 @@ _HERE = _Here()
 
 
 def _on(device, stream):
-    """Makes the tensors' device current, and ``stream`` where one is given."""
-    if stream is None and device.index == _device():
-        return _HERE
+    """Makes the tensors' device current, and ``stream`` where one is given (of that device: a stream of another one would
+    make that one current, and the kernels would run there)."""
+    if stream is None:
+        if device.index == _device():
+            return _HERE
+    elif stream.device != device:
+        _refuse(f"the stream is of another device ({stream.device}) than the tensors ({device})")
     both = contextlib.ExitStack()
     both.enter_context(torch.cuda.device(device))
     if stream is not None:
