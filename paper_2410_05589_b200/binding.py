@@ -10,6 +10,7 @@ import contextlib
 import ctypes as C
 import os
 import threading
+import warnings
 
 import torch
 
@@ -216,6 +217,8 @@ def verify_static(draft_tokens: torch.Tensor, draft_logits, target_logits: torch
 # ``status`` (int32, zeroed by the caller) has bit 1 set by a call whose device-side wait expired; calls without one report to
 # a word of the device that ``train_poll`` reads.  With ``stream`` the caller orders it behind what wrote the inputs, and keeps
 # inputs and outputs until it is done with them, as with any tensor that is used on another stream than its own.
+# Outputs are values without an autograd graph: a step calls the ``*_backward`` functions, itself or from a
+# torch.autograd.Function whose forward and backward call the two.
 _DTYPE_CODE = {torch.float32: PS_DTYPE_F32, torch.bfloat16: PS_DTYPE_BF16}
 
 
@@ -311,6 +314,17 @@ def _scratch(nbytes, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None   # (0: the call says why)
 
 
+def _values_only(name, *tensors):
+    """Says so where autograd would stop at the outputs without a word (not within a Function, nor under no_grad)."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                warnings.warn(f"{name}: the outputs carry no autograd graph although an input requires a gradient; call {name}_backward "
+                              f"for it, from a torch.autograd.Function for instance (under torch.no_grad() this is not said)",
+                              stacklevel=3)
+                return
+
+
 def _check_status(status, device):
     if status is not None:
         _tensors(device, status, dtype=torch.int32)
@@ -360,8 +374,10 @@ def group_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_ctx, n_
 
     q [group rows][n_heads][head_dim]; k, v [context and group rows][n_kv_heads][head_dim], float32 or bfloat16, views
     with a larger row stride allowed; n_ctx, n_groups: host lists, one entry per sequence; scale: head_dim ** -0.5 by
-    default.  Returns ``out`` (like q) and ``lse`` [n_heads][group rows] float32; ``out`` may carry them preallocated.
+    default.  Returns ``out`` (like q) and ``lse`` [n_heads][group rows] float32, without an autograd graph; ``out`` may carry
+    them preallocated.
     """
+    _values_only("group_attention", q, k, v)
     a, device, wq, _ = _group_args(q, k, v, n_ctx, n_groups, k_masks, scale)
     lib = load_library()
     with _on(device, stream):
@@ -439,7 +455,8 @@ def lm_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, out: dict | 
 
     x [rows][hidden] (a view with a larger row stride allowed), w [vocab][hidden], float32 or bfloat16; labels [rows]
     int32, any value outside the vocabulary (-100) for rows that count for nothing.  Returns ``loss`` and ``lse``
-    [rows] float32, 0 for those rows."""
+    [rows] float32, 0 for those rows, without an autograd graph."""
+    _values_only("lm_loss", x, w)
     device, size = _loss_args(x, w, labels)
     lib = load_library()
     with _on(device, stream):
@@ -491,7 +508,8 @@ def embed_rows(ids: torch.Tensor, table: torch.Tensor, mask_rows=None, scale: fl
                stream=None) -> torch.Tensor:
     """ps_embed_rows: scaled rows of table [vocab][hidden] (ids below vocab) and of mask_rows [k_masks][hidden] (ids from
     vocab on); any other id gives a row of zeros.  ids [rows] int32; ``out`` [rows][hidden] may be a view with a
-    larger row stride, such as the embedding half of the fc layer's input."""
+    larger row stride, such as the embedding half of the fc layer's input.  The result carries no autograd graph."""
+    _values_only("embed_rows", table, mask_rows)
     device, code = _first(table, "table")
     _tensors(device, mask_rows, out, dtype=table.dtype)
     _tensors(device, ids)
