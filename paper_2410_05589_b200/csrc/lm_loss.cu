@@ -201,7 +201,8 @@ __global__ void __launch_bounds__(256) k_loss_join(int tiles, LossBuf b, float* 
     for (int e = 0; e < 4; ++e) p[e] = t0 + 32 * e < tiles ? part[t0 + 32 * e] : make_float2(-INFINITY, 0.f);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      nan |= p[e].y != p[e].y;
+      // (a sum of nothing against a maximum: log2(e) times it was beyond single precision, from 2.36e38 on)
+      nan |= p[e].y != p[e].y || (p[e].y == 0.f && p[e].x > -INFINITY);
       if (p[e].x > m) {
         s = s * exp2f((m - p[e].x) * kLog2e) + p[e].y;
         m = p[e].x;
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(256) k_loss_join(int tiles, LossBuf b, float* 
     // s has all but the label's logit (vocab = 1: nothing).  lse is that of the logits as the product formed them, which the
     // backward call forms again; the loss takes the label's in single precision.
     const float rest = top + logf(s), own = b.own[i], picked = b.picked[i], high = fmaxf(own, rest);
-    const float d = rest - picked, e = log1pf(expf(-fabsf(d)));
+    const float d = (top - picked) + logf(s), e = log1pf(expf(-fabsf(d)));
     const int r = b.row_of[i];
     lse[r] = high == -INFINITY && own == rest ? high : high + log1pf(expf(-fabsf(own - rest)));
     loss[r] = picked == INFINITY ? NAN : (d > 0.f ? d + e : e);     // (inf - inf: no number, like every other logit of +inf)

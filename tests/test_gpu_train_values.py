@@ -109,6 +109,26 @@ def test_loss_of_extreme_logits(ps, dtype):
     assert ((loss[[3, 5]] - want).abs() <= 1e-4).all()
 
 
+@TYPES
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_loss_of_logits_at_the_end_of_single_precision(ps, sign, dtype):
+    """Logits of 3e38, whose products with log2(e) are beyond it: the loss is right, or it says that it is not."""
+    V, H = 600, 64
+    w, x = torch.zeros((V, H), dtype=dtype, device="cuda"), torch.zeros((4, H), dtype=dtype, device="cuda")
+    x[:, 0] = 2.0 ** 126
+    w[300, 0] = sign * 3.5          # a logit of +-2.98e38; the others are 0 ...
+    w[:, 1] = sign * 3.5
+    x[2:, 1] = 2.0 ** 126           # ... or all of them are that
+    x[2:, 0] = 0
+    labels = torch.tensor([5, 300, 5, 300], dtype=torch.int32, device="cuda")
+    r = ps.lm_loss(x, w, labels)
+    big = 3.5 * 2.0 ** 126
+    want = [math.log(V - 1), big, math.log(V), math.log(V)] if sign < 0 else [big, 0.0, math.log(V), math.log(V)]
+    for got, right in zip(r["loss"].tolist(), want):
+        # (an ulp of the logit where all of the loss is a difference of such: 2^103)
+        assert not math.isfinite(got) or abs(got - right) <= 1e-5 + 1e-6 * right, (got, right)
+
+
 # ---- a step that has diverged -----------------------------------------------------------------------------------
 
 def times(fn, n):
