@@ -4,16 +4,18 @@
 // where T is the token table with the [MASK] rows behind it.
 //
 // Both are bound by memory.  Forward: a warp per piece of a row, eight 16-byte vectors a lane in flight.
-// Backward: the rows are put into the order of their ids (stable, so that every id's rows are added in
-// increasing order) and summed from that list; rows of the table that no id names, most of a large
+// Backward: the rows are put into the order of their ids (stable: an id's rows increase) and summed from that list in
+// pieces of 32 entries, whose sums are added in an order of their own, the same in every call; rows of the table that no id names, most of a large
 // vocabulary, are written as zeros meanwhile.
 //   k_embed_sort   a block per range of ids reads all of them once (40 KB for 10000 rows: they stay in L2),
 //                  counts those below its range, which is where its part of the list begins, and those
 //                  in it, per id and eighth of the rows; a second pass puts each eighth's rows in order.  No
 //                  block waits for another.  Then it writes its zero rows.
-//   k_embed_sum    a block per 32 entries of the list and run of columns; sums in single precision.  An id
+//   k_embed_sum    a block per 32 entries of the list and run of columns; sums in single precision, in the rows' order.  An id
 //                  whose rows all lie in the block is stored, the ends of longer ones become partial sums.
-//   k_embed_join   adds the partial sums of an id that crosses blocks, in order.
+//   k_embed_join   adds the partial sums of an id that crosses blocks: every eighth of those behind its first, then
+//                  the first and the eight sums.  Where the pieces begin depends on how many rows lower ids have
+//                  (a [MASK] row's gradient may differ in its last bits with and without the table's).
 // [MASK] ids name a row of every group (thousands of rows each): pieces of 32 keep them from being one
 // block's work.
 // Measured (with the launches' gaps): 10235 rows of 4096 bf16 forward 26 us (3.9 TB/s; most rows are [MASK] rows that come from
@@ -262,7 +264,7 @@ __global__ void k_embed_sum(int V, int H, const int* n_list, const Entry* __rest
 
 constexpr int kJoinWays = 8;
 // Block (slice, columns): where an id begins in the slice and goes on behind it, its partial sums; kJoinWays
-// threads a column, then their sums in order.
+// threads a column, each every kJoinWays-th of them, then their sums one after the other.
 template <class T, int N>
 __global__ void __launch_bounds__(32 * kJoinWays) k_embed_join(int V, int H, const int* n_list,
                                                                 const Entry* __restrict__ list, float scale,

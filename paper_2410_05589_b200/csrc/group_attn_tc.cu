@@ -42,6 +42,7 @@ typedef __nv_bfloat16 bf16;
 constexpr int kT = 128;                       // rows of a tile
 constexpr int kHalfBytes = kT * 128;          // 64 columns of a tile
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kFar = 1048576.f;             // (log2) of a reference: see the forward kernel
 constexpr float kSlack = 8.f;                 // a maximum this far (log2) above the reference forces a rescale
 
 template <int D>
@@ -566,7 +567,15 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
           }
         }
       }
-      const float ref = m > -INFINITY ? m * c : 0.f;
+      float ref = m > -INFINITY ? m * c : 0.f;
+      // (v c - ref is what ref's rounding left where the two are equal: nothing that counts up to kFar, and beyond single
+      // precision's exponents from 2^31 on)
+      if (__any_sync(0xffffffffu, fabsf(ref) > kFar)) {
+        const float far = m > -INFINITY ? m : 0.f;
+#pragma unroll
+        for (int j = 0; j < kT; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) - far);
+        ref = 0.f;
+      }
       f2 sum0 = {0.f, 0.f}, sum1 = {0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < kT; j += 32) {
@@ -624,7 +633,7 @@ k_gat_fwd(const __grid_constant__ Maps maps, const __grid_constant__ Seqs s, con
         }
       }
       if (r < rows) {
-        const float lse = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
+        const float lse = l == 0.f ? -INFINITY : fmaf(m, a.scale, log2f(l) * kLn2);
         if (t.splits == 1) a.lse[(size_t)u.h * a.rows + row] = lse;
         else t.part_l[at] = lse;
       }

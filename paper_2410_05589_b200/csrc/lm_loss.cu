@@ -201,8 +201,7 @@ __global__ void __launch_bounds__(256) k_loss_join(int tiles, LossBuf b, float* 
     for (int e = 0; e < 4; ++e) p[e] = t0 + 32 * e < tiles ? part[t0 + 32 * e] : make_float2(-INFINITY, 0.f);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      // (a sum of nothing against a maximum: log2(e) times it was beyond single precision, from 2.36e38 on)
-      nan |= p[e].y != p[e].y || (p[e].y == 0.f && p[e].x > -INFINITY);
+      nan |= p[e].y != p[e].y;
       if (p[e].x > m) {
         s = s * exp2f((m - p[e].x) * kLog2e) + p[e].y;
         m = p[e].x;
@@ -513,8 +512,15 @@ cudaError_t launch_rows(const LossArgs& a, const void* x, size_t ldx, const int*
   return launch_after(k_loss_gather<T>, dim3(p.rows_pad), dim3(256), 0, st, true, p.hidden, tile, (const T*)x, ldx, w, a.b, vec);
 }
 
-// Whether tiles of 64 rows are fewer than multiprocessors: then tiles of 32, whose steps take half as long (205 rows, 256 x 1000,
-// loss and gradients 98 -> 94 us).
+// Whether tiles of 64 rows are fewer than multiprocessors: then tiles of 32, whose steps take half as long.  Measured, tiles of 64
+// and of 32, us (a call alone in a graph; dx and dw each with the logits' gradient):
+//   rows x hidden x vocab   forward      dx            dw            tiles of 64: logits, dx (a part), dw
+//   64 x 256 x 1000         16.3 13.7    23.9 20.4     26.3 16.4     16, 4, 64
+//   205 x 256 x 1000        32.3 34.2    49.2 43.4     55.6 31.0     64, 16, 64
+//   330 x 320 x 1500        38.9 41.6    67.2 61.1     86.1 84.7     144, 30, 120
+//   1000 x 320 x 1500       41.4 44.0    106.6 105.5   158 179       384, 80, 120
+//   1000 x 768 x 5000       234 252      579 633       492 502       1264, 192, 948
+// (forward alone the line is at some 50 tiles; the backward call takes more of a step's time.)
 bool few_blocks(int tiles) { return tiles < device_sms(); }
 
 cudaError_t logits_fp32(const LossArgs& a, bool grad, int v0, int nv, cudaStream_t st) {

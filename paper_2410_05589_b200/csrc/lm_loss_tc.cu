@@ -45,6 +45,7 @@ constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr uint32_t kPeerMask = 0xFEFFFFFFu;      // shared::cluster address of the same offset in the leader CTA
 constexpr int kGroup = 8;                        // row tiles side by side
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kFar = 1048576.f;                // (log2) of a row's maximum
 
 enum Mode { FWD, GRAD, DX, DW };
 
@@ -267,9 +268,16 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
             if (j >= left) v[j] = -INFINITY;
             mx = fmaxf(mx, v[j]);
           }
-          const float l = mx > -INFINITY ? mx * kLog2e : 0.f;   // (nothing above -inf: the sum stays 0, or no number)
-          sum *= top > -INFINITY ? exp2f(top * kLog2e - l) : 0.f;
+          float l = mx > -INFINITY ? mx * kLog2e : 0.f;   // (nothing above -inf: the sum stays 0, or no number)
+          sum *= top > -INFINITY ? exp2f((top - mx) * kLog2e) : 0.f;
           top = mx;
+          // (v log2(e) - l is what l's rounding left where the two are equal: beyond single precision's exponents from 2^31 on)
+          if (__any_sync(0xffffffffu, fabsf(l) > kFar)) {
+            const float far = mx > -INFINITY ? mx : 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] -= far;
+            l = 0.f;
+          }
           float s0 = 0.f, s1 = 0.f;
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
