@@ -402,6 +402,10 @@ ps_status ps_verify_static(int vocab, int B, int n_draft, int n_target, const in
  * Common to all of them:
  *   - dtype is PS_DTYPE_F32 or PS_DTYPE_BF16: the storage type of every tensor marked `dtype`; sums,
  *     softmax statistics and losses are float.  Row strides (ld*) count elements.
+ *   - bf16: what is an operand of a product of the tensor cores is rounded to bf16 on its way there (half a step,
+ *     2^-8 relatively): the probabilities before P V and P^T dO, dS before dS K and dS^T Q, the logits' gradients
+ *     before g W and g^T x.  Outputs and gradients come out 2.2e-3 to 2.4e-3 off relatively where the rounding of the result
+ *     alone makes it 1.7e-3.
  *   - outputs overlap neither inputs nor each other.  Rows that belong to no sequence, and columns
  *     between a row's width and its stride, are left as they are.
  *   - results do not depend on what else runs, nor from one run to the next.
@@ -496,7 +500,9 @@ ps_status ps_lm_loss_backward(int dtype, int rows, int hidden, int vocab, const 
  *           scale * mask_rows[id-vocab]  vocab <= id < vocab + k_masks: the [MASK] rows (Sec. 4.3)
  *           0                            any other id (a padded row)
  *   d_table[v] = scale * sum of dout_r over the rows r with id v, d_mask likewise; rows of the table
- *   that no id names are set to 0.  The rows of an id are added in increasing order (in pieces of 32).
+ *   that no id names are set to 0.  The rows of an id are added in pieces of up to 32 in increasing order, the pieces' sums in
+ *   a fixed order.  Where the pieces begin depends on the rows of lower ids whose gradient is formed, so d_mask's last bits
+ *   may differ with and without d_table.
  *   ids      device [rows] int32;  out, dout device [rows][hidden] dtype, row strides ldo and lddo
  *   table, d_table device [vocab][hidden] dtype, mask_rows, d_mask device [k_masks][hidden] dtype, dense
  *   d_table, d_mask: either may be NULL: that gradient is not formed.  mask_rows may be NULL if k_masks = 0

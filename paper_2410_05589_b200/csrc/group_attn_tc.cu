@@ -4,8 +4,9 @@
 //   forward  S = Q K^T,  P = exp(S - max),  O += P V                 query rows on the 128 lanes
 //   dq       S = Q K^T,  dP = dO V^T,  dQ += dS K                    query rows on the lanes
 //   dk, dv   S^T = K Q^T,  dP^T = V dO^T,  dV += P^T dO,  dK += dS^T Q   keys on the lanes (masks: see k_gat_masks)
-// with dS = P (dP - delta).  P and dS are rounded to bf16, the operand type of the products that read them (the sums are
-// fp32); they go from registers to tensor memory and are read there as the products' A operand, so that
+// with dS = P (dP - delta).  P and dS are rounded to bf16, the operand type of the products that read them (an MMA has both
+// operands of one type, and V, K, Q and dO are bf16; a second, low half of P would be half as many products again).  The sums are
+// fp32: out and the gradients are 2.3e-3 off where the rounding of the result alone makes it 1.7e-3.  They go from registers to tensor memory and are read there as the products' A operand, so that
 // shared memory holds nothing but Q, K, V and dO, which tiled TMA brings in the one layout (rows of 64 values,
 // 128-byte swizzle) that serves a product over head_dim (K-major) and one over rows (MN-major).
 //
@@ -383,11 +384,13 @@ __device__ __forceinline__ void alloc_tmem(uint32_t* where, int cols) {
 // Two blocks an SM, each with one query tile of a head: one's softmax runs beside the other's products.  Warp 0 issues
 // the TMA loads, warp 1 the MMAs, warps 2..5 own a row a thread.  S of the next key tile is issued behind O += P V of this
 // one (P lies in S's columns: the tensor cores work in order); K and V pass through a ring.
-// Measured (52 heads, 2 sequences, k = 8): 450 us.  One persistent block an SM with two query tiles that share the ring: four
+// Measured (52 heads, 2 sequences, k = 8, 319 steps of 128 keys an SM): 450 us by itself, 500 in calls back to back, where the power
+// limit takes the clock down.  By themselves too: one persistent block an SM with two query tiles that share the ring, four
 // warps a tile 510, eight 541, steps of 64 keys with two buffers of scores 639 (an MMA of 64 columns takes as long as one of
-// 128).  A quarter of the exponentials as polynomials on the FMA units: 485.
-// What bounds it: of 2000 cycles a step and tile the MMAs are 1024 and the exponentials (16 a cycle) as many; the rest is the
-// latency of the two hand-overs between the warps and the tensor cores, which two blocks hide by half.
+// 128); a quarter of the exponentials as polynomials on the FMA units 485.
+// What bounds it: of 2400 cycles a step and SM (3300 where a query tile has five steps: 13B heads, 4 sequences of 213-420
+// groups) the MMAs are 1024 and the exponentials (16 a cycle) as many; the rest is the latency of the two hand-overs between
+// the warps and the tensor cores, which the second block hides in part, and a query tile's beginning and end.
 template <int D>
 struct Fwd {
   static constexpr int NS = D == 128 ? 2 : 4;   // slots of the ring
@@ -681,9 +684,9 @@ __global__ void __launch_bounds__(256) k_gat_join(const __grid_constant__ AttnAr
 // the keys each.  The scores pass through registers, so that the next tile's are formed as soon as they are read; dP has
 // two buffers, and dS takes dP's columns (each quarter its own): the tensor cores work on S, dP of the next tile and dQ of the
 // last one while the warps turn this one's into dS.
-// Measured: 13B heads, 4 sequences of 150-420 groups of 5 rows, 177 us; 2047 groups on 8 key heads 305.  Steps of 64 keys in three
-// buffers, two groups of warps taking turns: 217 and 427.  What bounds it: 3300 cycles a step of which the MMAs are 1536
-// and the exponentials 1024; the rest is the latency of the loads from tensor memory, stores to it and barriers.
+// Measured: 13B heads, 4 sequences of 213-420 groups of 5 rows, 187 us; 2047 groups on 8 key heads 315.  Steps of 64 keys in three
+// buffers, two groups of warps taking turns: a fifth and two fifths more.  What bounds it: 3950 and 3100 cycles a step of which the
+// MMAs are 1536 and the exponentials 1024; the rest is the latency of the loads from tensor memory, stores to it and barriers.
 template <int D>
 struct Dq {
   static constexpr int NK = 3, NV = 2, threads = 576;
@@ -928,7 +931,7 @@ __global__ void __launch_bounds__(256) k_gat_dq_join(const __grid_constant__ Att
 // A [MASK] row is seen by the R - j rows of its own group that follow it: too little for a matrix product.  A warp per
 // (group, key head) keeps the group's keys, values and their gradients in registers, a lane D / 32 neighbouring
 // channels; it also forms delta = dout . out of the rows it reads anyway.
-// Measured: 6650 rows of 40 heads 110 us (409 MB, 3.7 TB/s); 10235 rows of 32 heads on 8, 89 us.  Bound by the latency of a
+// Measured: 6650 rows of 40 heads 121 us (409 MB, 3.4 TB/s); 10235 rows of 32 heads on 8, 98 us.  Bound by the latency of a
 // warp's loads: its registers leave room for 12 warps an SM (with spills at 16 and 20 it took 129 and 136 us).
 // delta of the rows with few keys (see kExactKeys): the first groups of sequences with a short context.  A warp per (row, head).
 __host__ __device__ inline int few_groups(int ctx, int groups) { return ctx >= kExactKeys ? 0 : (groups < kExactKeys - ctx ? groups : kExactKeys - ctx); }
@@ -1075,9 +1078,9 @@ k_gat_masks(const __grid_constant__ Seqs s, const __grid_constant__ AttnArgs a, 
 // in its columns), dK and dV.  The warps form P^T while the tensor cores work on dK and dP^T, and dS^T while they work on
 // dV and the next step's S^T.  A thread owns a key and a quarter of the query columns, whose lse and delta a
 // warp of its own puts into shared memory.
-// Measured: 13B heads, 4 sequences of 150-420 groups of 5 rows, 185 us; 2047 groups on 8 key heads 326, in one part per key tile
+// Measured: 13B heads, 4 sequences of 213-420 groups of 5 rows, 187 us; 2047 groups on 8 key heads 329, in one part per key tile
 // 576 (the first tiles are seen by all 10235 rows of four heads, the last ones by few).  Steps of 64 rows with two groups of
-// warps taking turns: 224 and 405.  What bounds it: 4500 cycles a step, of which the MMAs are 2048; tensor memory has no room
+// warps taking turns: a fifth and a quarter more.  What bounds it: 5000 and 3650 cycles a step, of which the MMAs are 2048; tensor memory has no room
 // for a second step's scores of 128 rows, so that the two halves of a step wait for each other's products.
 template <int D>
 struct Dkv {
@@ -1443,7 +1446,7 @@ __global__ void __launch_bounds__(256) k_gat_dkv_join(const __grid_constant__ Se
 // little more than another.  What costs is a value that reaches rows or keys by its place in a tile alone, or a part of
 // the columns.  Measured (2047 groups of 5 rows, 32 heads on 8; forward and backward 0.24 + 0.77 ms): all of dout, q or k NaN
 // 0.24 + 0.87, all of v 1.1 + 0.87; one NaN early in dout or q 0.24 + 17 (119 keys a head over all 40940 rows), in v 22 +
-// 0.85 (all rows over all keys), in k 0.24 + 0.84.  Without one this launch takes 2 us.
+// 0.85 (all rows over all keys), in k 0.24 + 0.84.  Without one this launch takes 5 us by itself, 2 to 3 in a call.
 template <int D>
 __device__ __noinline__ void row_again(const Seqs& s, const AttnArgs& a, int qr, int h) {
   constexpr int C = D / 32;
