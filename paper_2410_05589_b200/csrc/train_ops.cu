@@ -57,7 +57,11 @@ using namespace ps::train;
 extern "C" ps_status ps_train_poll(void* stream) {
   cudaStream_t st = (cudaStream_t)stream;
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-  if (cudaStreamIsCapturing(st, &capture) == cudaSuccess && capture != cudaStreamCaptureStatusNone) return PS_ERR_INVALID_ARG;
+  const cudaError_t asked = cudaStreamIsCapturing(st, &capture);
+  if (asked != cudaSuccess || capture != cudaStreamCaptureStatusNone) {
+    (void)cudaGetLastError();
+    return PS_ERR_INVALID_ARG;
+  }
   int words[2] = {0, 0};
   cudaError_t e = attn_take_status(&words[0], st);
   if (e == cudaSuccess) e = loss_take_status(&words[1], st);

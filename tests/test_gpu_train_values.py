@@ -130,14 +130,17 @@ def test_loss_of_logits_at_the_end_of_single_precision(ps, sign, dtype):
 
 
 @pytest.mark.parametrize("n_ctx, n_groups", [([30], [20]), ([500], [3]), ([0, 60], [70, 40])], ids=["one part", "several parts", "two sequences"])
+@pytest.mark.parametrize("d, odd", [(64, False), (128, False), (128, True)], ids=["64", "128", "128 odd"])
 @TYPES
-def test_scores_far_from_zero(ps, n_ctx, n_groups, dtype):
-    """Scores of 1e10 to 1e12, exact in every type and 2^29 apart: the largest one that a row sees has all of the weight."""
-    k, nh, d = 1, 2, 64
+def test_scores_far_from_zero(ps, n_ctx, n_groups, d, odd, dtype):
+    """Scores of 1e10 to 1e12, more than 2^28 apart: the largest one that a row sees has all of the weight."""
+    k, nh = 1, 2
     R = k + 1
     q, kk, v, do = attn_inputs(91, n_ctx, n_groups, k, nh, nh, d, dtype)
     q.zero_(), kk.zero_()
     q[..., 0] = 2.0 ** 20
+    if odd:
+        v = torch.empty(v.numel() + 1, dtype=dtype, device="cuda")[1:].view(v.shape).copy_(v)
     n = kk.shape[0]
     sizes = (128 + torch.arange(128)[None, :]).double() * 2.0 ** torch.arange(5)[:, None]     # 640 different ones
     order = torch.randperm(640, generator=torch.Generator().manual_seed(4))[:n]
