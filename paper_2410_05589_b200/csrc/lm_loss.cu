@@ -193,6 +193,8 @@ __global__ void __launch_bounds__(256) k_loss_join(int tiles, LossBuf b, float* 
   const int i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (i >= *b.n) return;
   const float2* part = b.part + (size_t)i * tiles;
+  const float own = b.own[i], picked = b.picked[i];
+  const int r = b.row_of[i];
   float m = -INFINITY, s = 0.f;
   bool nan = false;
   for (int t0 = lane; t0 < tiles; t0 += 128) {
@@ -217,14 +219,17 @@ __global__ void __launch_bounds__(256) k_loss_join(int tiles, LossBuf b, float* 
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (__any_sync(0xffffffffu, nan)) s = NAN;
-  if (lane == 0) {
-    // s has all but the label's logit (vocab = 1: nothing).  lse is that of the logits as the product formed them, which the
-    // backward call forms again; the loss takes the label's in single precision.
-    const float rest = top + logf(s), own = b.own[i], picked = b.picked[i], high = fmaxf(own, rest);
-    const float d = (top - picked) + logf(s), e = log1pf(expf(-fabsf(d)));
-    const int r = b.row_of[i];
-    lse[r] = high == -INFINITY && own == rest ? high : high + log1pf(expf(-fabsf(own - rest)));
-    loss[r] = picked == INFINITY ? NAN : (d > 0.f ? d + e : e);     // (inf - inf: no number, like every other logit of +inf)
+  if (lane < 2) {
+    // s has all but the label's logit (vocab = 1: nothing).  Lane 1: lse, that of the logits as the product formed them, which the
+    // backward call forms again.  Lane 0: the loss, with the label's logit in single precision.  Both are
+    // log(exp x + exp y) = max(x, y) + log(1 + exp(-|x - y|)), the loss with y = 0.
+    const float log_s = logf(s), rest = top + log_s, d = lane ? rest - own : (top - picked) + log_s, e = log1pf(expf(-fabsf(d)));
+    if (lane) {
+      const float high = fmaxf(own, rest);
+      lse[r] = high == -INFINITY && own == rest ? high : high + e;
+    } else {
+      loss[r] = picked == INFINITY ? NAN : (d > 0.f ? d + e : e);     // (inf - inf: no number, like every other logit of +inf)
+    }
   }
 }
 

@@ -47,6 +47,11 @@ constexpr uint32_t kPeerMask = 0xFEFFFFFFu;      // shared::cluster address of t
 constexpr int kGroup = 8;                        // row tiles side by side
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = 1048576.f;                // (log2) of a row's maximum
+// k blocks (of 64) that a logit is summed over on the tensor cores: longer rows are summed in parts of equal size, which the FMA
+// units add.  The tensor cores truncate, and what that takes from a logit is in proportion to it and to the length of the chain:
+// lse of 6656 terms came out 1.5e-6 off relatively, in two parts 7.2e-7 (4096 in one: 5.7e-7; parts of 1024: 1.2e-7 to 1.9e-7, for 2
+// to 5 % of the product's time).
+constexpr int kChain = 64;
 
 enum Mode { FWD, GRAD, DX, DW };
 
@@ -112,6 +117,16 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
+  uint32_t r[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(
+          r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
 // Shared-memory operand of 128 rows (or columns).  K-major: as umma::smem_desc.  MN-major: k rows of 64 values (128
 // bytes, swizzled), the second 64 values 64 k rows further on, groups of 8 k rows 1024 bytes apart.
 template <bool MN>
@@ -131,7 +146,35 @@ __device__ __forceinline__ void tile_at(int t, int m_tiles, int n_tiles, int& m,
   m = g * kGroup + i - n * rows;
 }
 
-template <int MODE>
+// A tile of logits in several accumulators, one behind the other: sums a thread's 128 columns of them in its registers and leaves
+// the result in the last one; c, the number of the first, becomes that one's.
+__device__ __forceinline__ bool add_chains(Ctl& ctl, uint32_t lanes, int chains, int& c, volatile int* abort_flag) {
+  float v[128];
+#pragma unroll
+  for (int j = 0; j < 128; ++j) v[j] = 0.f;
+  for (int i = 1;; ++i, ++c) {
+    if (!__all_sync(0xffffffffu, mbar_wait(&ctl.acc_full[c & 1], (c >> 1) & 1, abort_flag))) return false;
+    fence_after_sync();
+#pragma unroll
+    for (int j0 = 0; j0 < 128; j0 += 16) {
+      const uint32_t at = lanes + (c & 1) * kTile + j0;
+      float x[16];
+      umma::tmem_ld16(at, x);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j0 + j] += x[j];
+      if (i == chains) tmem_st16(at, v + j0);
+    }
+    if (i == chains) break;
+    fence_before_sync();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) arrive_leader(&ctl.acc_empty[c & 1]);
+  }
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+  return true;
+}
+
+// PARTS: of logits that are summed in several parts.
+template <int MODE, bool PARTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUtensorMap tB, const __grid_constant__ Args a) {
   constexpr bool A_MN = MODE == DW, B_MN = MODE == DX || MODE == DW;
@@ -170,7 +213,8 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
   const int kb = MODE == DW ? (n + kBK - 1) / kBK : a.kb;
   const int splits = MODE == DX ? dx_splits(n, a.hidden, a.kb_piece, n_pairs) : 1;
   const int tiles = m_tiles * n_tiles * splits;
-  // Tile t: its place, and its part of the k blocks.
+  const int chains = PARTS ? (kb + kChain - 1) / kChain : 1, parts = MODE == DX ? splits : chains;
+  // Tile t: its place, and (dx) its part of the k blocks.
   auto place = [&](int t, int& m, int& nn, int& part) {
     part = MODE == DX ? t / (m_tiles * n_tiles) : 0;
     tile_at(t - part * m_tiles * n_tiles, m_tiles, n_tiles, m, nn);
@@ -212,26 +256,29 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
       int st = 0, c = 0;
       uint32_t parity = 0;
       bool alive = true;
-      for (int t = pair; alive && t < tiles; t += n_pairs, ++c) {
-        const int buf = c & 1;
-        if (!mbar_wait(&ctl.acc_empty[buf], ((c >> 1) & 1) ^ 1, abort_flag)) break;
-        fence_after_sync();
-        const uint32_t d = tmem + buf * kTile;
+      for (int t = pair; alive && t < tiles; t += n_pairs) {
         int m, nn, part;
         place(t, m, nn, part);
-        const int k0 = kb * part / splits, k1 = kb * (part + 1) / splits;
-        for (int k = k0; k < k1; ++k) {
-          if (!mbar_wait(&ctl.full[st], parity, abort_flag)) { alive = false; break; }
+        for (int i = 0; alive && i < chains; ++i, ++c) {
+          const int buf = c & 1, at = MODE == DX ? part : i;
+          alive = mbar_wait(&ctl.acc_empty[buf], ((c >> 1) & 1) ^ 1, abort_flag);
+          if (!alive) break;
           fence_after_sync();
-          const uint32_t sa = base + st * kStageBytes;
-          const uint64_t da = op_desc<A_MN>(sa), db = op_desc<B_MN>(sa + kOpBytes);
+          const uint32_t d = tmem + buf * kTile;
+          const int k0 = kb * at / parts, k1 = kb * (at + 1) / parts;
+          for (int k = k0; k < k1; ++k) {
+            if (!mbar_wait(&ctl.full[st], parity, abort_flag)) { alive = false; break; }
+            fence_after_sync();
+            const uint32_t sa = base + st * kStageBytes;
+            const uint64_t da = op_desc<A_MN>(sa), db = op_desc<B_MN>(sa + kOpBytes);
 #pragma unroll
-          for (int s = 0; s < kBK / 16; ++s)
-            mma_pair(d, da + s * (A_MN ? 128 : 2), db + s * (B_MN ? 128 : 2), id, k > k0 || s > 0);
-          commit_pair(&ctl.empty[st]);
-          if (++st == kStages) { st = 0; parity ^= 1; }
+            for (int s = 0; s < kBK / 16; ++s)
+              mma_pair(d, da + s * (A_MN ? 128 : 2), db + s * (B_MN ? 128 : 2), id, k > k0 || s > 0);
+            commit_pair(&ctl.empty[st]);
+            if (++st == kStages) { st = 0; parity ^= 1; }
+          }
+          if (alive) commit_pair(&ctl.acc_full[buf]);
         }
-        if (alive) commit_pair(&ctl.acc_full[buf]);
       }
     }
   } else {
@@ -239,15 +286,17 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
     const int q = warp & 3, half = (warp - 2) >> 2, r = 32 * q + lane;
     int c = 0;
     for (int t = pair; t < tiles; t += n_pairs, ++c) {
-      const int buf = c & 1;
       int mt, nt, part;
       place(t, mt, nt, part);
       const int m = mt * kTile + (int)rank * 128 + r, c0 = nt * kTile + half * 128;
       const int own = MODE == FWD ? a.b.label[m] - c0 : -1;   // the label's column of these 128
-      const bool ok = kb == 0 || mbar_wait(&ctl.acc_full[buf], (c >> 1) & 1, abort_flag);
+      const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16) + half * 128;
+      if (PARTS && !add_chains(ctl, lanes, chains, c, abort_flag)) break;
+      const int buf = c & 1;
+      const bool ok = PARTS || kb == 0 || mbar_wait(&ctl.acc_full[buf], (c >> 1) & 1, abort_flag);
       if (!__all_sync(0xffffffffu, ok)) break;
       fence_after_sync();
-      const uint32_t ta = tmem + ((uint32_t)(32 * q) << 16) + buf * kTile + half * 128;
+      const uint32_t ta = lanes + buf * kTile;
       if (MODE == FWD) {
         float top = -INFINITY, sum = 0.f;
 #pragma unroll 1
@@ -255,14 +304,6 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
           float v[32];
           tmem_ld32(ta + j0, v);
           const int left = a.cols - c0 - j0;
-          if (__any_sync(0xffffffffu, own >= j0 && own < j0 + 32)) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (j0 + j == own) {
-                a.b.own[m] = v[j];
-                v[j] = -INFINITY;
-              }
-          }
           float mx = top;
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
@@ -270,15 +311,28 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
             mx = fmaxf(mx, v[j]);
           }
           float l = mx > -INFINITY ? mx * kLog2e : 0.f;   // (nothing above -inf: the sum stays 0, or no number)
+          const bool here = own >= j0 && own < j0 + 32;
+          if (__any_sync(0xffffffffu, here || fabsf(l) > kFar)) {
+            float x = 0.f;
+            mx = top;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              if (j0 + j == own) {
+                x = v[j];
+                v[j] = -INFINITY;
+              }
+              mx = fmaxf(mx, v[j]);
+            }
+            if (here) a.b.own[m] = x;
+            // (v log2(e) - l is what l's rounding left where the two are equal: beyond single precision's exponents from 2^31 on)
+            const bool far = fabsf(mx > -INFINITY ? mx * kLog2e : 0.f) > kFar;
+            l = mx > -INFINITY && !far ? mx * kLog2e : 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (far) v[j] -= mx;
+          }
           sum *= top > -INFINITY ? exp2f((top - mx) * kLog2e) : 0.f;
           top = mx;
-          // (v log2(e) - l is what l's rounding left where the two are equal: beyond single precision's exponents from 2^31 on)
-          if (__any_sync(0xffffffffu, fabsf(l) > kFar)) {
-            const float far = mx > -INFINITY ? mx : 0.f;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] -= far;
-            l = 0.f;
-          }
           float s0 = 0.f, s1 = 0.f;
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
@@ -376,13 +430,21 @@ k_loss_gemm(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUte
   }
 }
 
-template <int MODE>
-cudaError_t launch(const CUtensorMap& tA, const CUtensorMap& tB, const Args& g, int most_tiles, cudaStream_t st) {
+template <int MODE, bool PARTS>
+cudaError_t launch_as(const CUtensorMap& tA, const CUtensorMap& tB, const Args& g, int most_tiles, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = allow_smem((const void*)k_loss_gemm<MODE>, kSmem, done);
+  cudaError_t e = allow_smem((const void*)k_loss_gemm<MODE, PARTS>, kSmem, done);
   if (e != cudaSuccess) return e;
   const int pairs = std::min(most_tiles, device_sms() / 2);
-  return launch_after(k_loss_gemm<MODE>, dim3(2 * pairs), dim3(kThreads), kSmem, st, true, tA, tB, g);
+  return launch_after(k_loss_gemm<MODE, PARTS>, dim3(2 * pairs), dim3(kThreads), kSmem, st, true, tA, tB, g);
+}
+template <int MODE>
+cudaError_t launch(const CUtensorMap& tA, const CUtensorMap& tB, const Args& g, int most_tiles, cudaStream_t st) {
+  // (two kernels: the sums of several parts take 168 registers a thread, with which a block does not start beside those of the
+  // kernel before it: 2 us of a call)
+  if constexpr (MODE == FWD || MODE == GRAD)
+    if (g.kb > kChain) return launch_as<MODE, true>(tA, tB, g, most_tiles, st);
+  return launch_as<MODE, false>(tA, tB, g, most_tiles, st);
 }
 
 Args common(const LossArgs& a) {

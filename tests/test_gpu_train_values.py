@@ -129,6 +129,21 @@ def test_loss_of_logits_at_the_end_of_single_precision(ps, sign, dtype):
         assert abs(got - right) <= 4 * ref.W * right, (got, right)
 
 
+def test_logits_of_long_rows(ps):
+    """32768 positive terms a logit.  The tensor cores truncate as they add: a part of 4096 terms is 256 steps, each of which takes
+    less than an ulp (2^-23) of what is there, which grows evenly to the part's size; so 128 ulps of the logit in all, and one for
+    each part that is added.  In one chain it would be some 370 (0.36 ulps a step)."""
+    rows, H, V = 5, 32768, 40
+    g = torch.Generator().manual_seed(8)
+    x, w = (((torch.rand((n, H), generator=g) + 0.5) * s).bfloat16() for n, s in ((rows, 0.01), (V, 0.02)))
+    labels = torch.arange(rows, dtype=torch.int32)
+    got = ps.lm_loss(x.cuda(), w.cuda(), labels.cuda())
+    S = x.double() @ w.double().T
+    lse = torch.logsumexp(S, -1)
+    off = (got["lse"].double().cpu() - lse).abs()
+    assert (off <= (128 + 8) * ref.W * S.amax(-1) + (V + 8) * ref.W + 4 * ref.W * lse).all(), (off / S.amax(-1) / ref.W).tolist()
+
+
 @pytest.mark.parametrize("n_ctx, n_groups", [([30], [20]), ([500], [3]), ([0, 60], [70, 40])], ids=["one part", "several parts", "two sequences"])
 @pytest.mark.parametrize("d, odd", [(64, False), (128, False), (128, True)], ids=["64", "128", "128 odd"])
 @TYPES
